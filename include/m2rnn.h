@@ -233,6 +233,11 @@ m2rnn_status m2rnn_bwd_opt(const m2rnn_desc *desc, const m2rnn_opts *opts, const
  *   paper prints none)   dw [C,4] fp32   dbias [C] fp32 or NULL.   C: a multiple of 8.
  *   workspace: m2rnn_conv_silu_workspace_bytes(B, T, C) bytes (backward only).
  *
+ *   m2rnn_conv_silu_window_fwd goes on where a sequence stopped (a token of serving, the next
+ *   segment of a prompt): the three steps in front of the first are the rows of win [B,3,C] io
+ *   (oldest first; NULL: zeros) and the last three go to win_out [B,3,C] (NULL: not wanted; may
+ *   be win).  T = 0 hands the window on.  The backward belongs to sequences that start from zeros.
+ *
  * Epilogue of y:  out = RMSNorm(y (.) g), g = SiLU(a), a the output gate's pre-activation:
  *   x_i = y_i g_i,  s = 1 / sqrt(mean_i x_i^2 + eps),  out_i = w_i x_i s   over ALL D = N V
  *   features of a token (the "RMSNormTP Module" appendix normalises over the features of all
@@ -250,6 +255,9 @@ m2rnn_status m2rnn_bwd_opt(const m2rnn_desc *desc, const m2rnn_opts *opts, const
 size_t m2rnn_conv_silu_workspace_bytes(int32_t B, int32_t T, int32_t C);
 m2rnn_status m2rnn_conv_silu_fwd(int32_t B, int32_t T, int32_t C, int32_t io, const void *x,
                                  const void *w, const void *bias, void *out, void *hip_stream);
+m2rnn_status m2rnn_conv_silu_window_fwd(int32_t B, int32_t T, int32_t C, int32_t io, const void *x,
+                                        const void *w, const void *bias, const void *win, void *out,
+                                        void *win_out, void *hip_stream);
 m2rnn_status m2rnn_conv_silu_bwd(int32_t B, int32_t T, int32_t C, int32_t io, const void *x,
                                  const void *w, const void *bias, const void *dout, void *dx,
                                  float *dw, float *dbias, void *workspace, size_t workspace_bytes,
@@ -262,6 +270,72 @@ m2rnn_status m2rnn_gated_rmsnorm_bwd(int32_t B, int32_t T, int32_t D, int32_t io
                                      const void *a, const void *w, float eps, const float *s,
                                      const void *dout, void *dy, void *da, float *dw,
                                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Group norm of a token's channels with an activation, channels last.  The D channels of a token are
+ * `groups` groups of L = D / groups neighbours (a head each); every token and group on its own
+ *     mu = mean x, or 0 without M2RNN_NORM_CENTER,   s = 1 / sqrt(mean (x - mu)^2 + eps),
+ *     n = w (x - mu) s + b,
+ *     out = n,   SiLU(n) with M2RNN_NORM_SILU,   or n SiLU(a) where a is given (not both).
+ * Behind a scan: y [B,T,N V] with groups = N and the output gate's pre-activation as a.  In front of the
+ * gated delta rule: q and k of unit length are groups of K channels, no centring, w = K^{-1/2} everywhere.
+ *   x, out, dout, dx, a, da [B,T,D] io; a NULL: no gate.   w, b [D] io; NULL: 1, 0.
+ *   dw, db [D] fp32: gradients of w and b (of a w of ones, a b of zeros where those are NULL),
+ *   overwritten, summed over (b, t) in a fixed order; NULL: not wanted.
+ *   mode: M2RNN_NORM_* or'ed.   L: a multiple of 8, at most 1024.   eps >= 0.
+ *   workspace: m2rnn_group_norm_workspace_bytes(B, T, D) bytes, for dw and db only.
+ *   out may be x or a, dx may be x or dout, da may be a or dout or x, as long as no two outputs are
+ *   the same buffer: a token's inputs are read before its outputs are written.
+ * Errors as above; M2RNN_ERR_SHAPE also for a mode that does not exist.
+ */
+enum { M2RNN_NORM_CENTER = 1, M2RNN_NORM_SILU = 2 };
+size_t m2rnn_group_norm_workspace_bytes(int32_t B, int32_t T, int32_t D);
+m2rnn_status m2rnn_group_norm_fwd(int32_t B, int32_t T, int32_t D, int32_t groups, int32_t io, int32_t mode,
+                                  const void *x, const void *a, const void *w, const void *b, float eps, void *out,
+                                  void *hip_stream);
+m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t groups, int32_t io, int32_t mode,
+                                  const void *x, const void *a, const void *w, const void *b, float eps,
+                                  const void *dout, void *dx, void *da, float *dw, float *db, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gated delta rule: the linear matrix-state layer that hybrids put beside this one.  For every batch
+ * element and head, with a state H in R^{K x V}:
+ *     Hd_t = e^{g_t} H_{t-1},   u_t = beta_t (v_t - Hd_t^T k_t),   H_t = Hd_t + k_t u_t^T,   y_t = H_t^T q_t.
+ * The descriptor is the scan's (chunk and flags 0), with V also 256.
+ *   q, k  [B,T,Nqk,K] io      v [B,T,N,V] io      g [B,T,N] fp32, log of the gate, <= 0 (-inf: a reset)
+ *   beta  [B,T,N] fp32        H0 [B,N,K,V] fp32 or NULL (zero)
+ *   y     [B,T,N,V] io, out   HT [B,N,K,V] fp32, out, or NULL; may be H0
+ *   ckpt  out, m2rnn_delta_ckpt_bytes() bytes, for a later m2rnn_delta_bwd of the same descriptor; NULL
+ *         where none follows.  What it holds is the library's own.
+ * k is used as it is: with beta_t |k_t|^2 <= 2 the rule does not expand, e.g. keys of unit length
+ * (m2rnn_group_norm_fwd) and beta in [0, 2].  A step with g = 0 and beta = 0 leaves the state as it was: so
+ * are sequences of a batch padded at their end (q, k, v of the padding finite, their y to be ignored).
+ * Without checkpoints a forward of few steps runs the recurrence step by step in one launch and needs no
+ * workspace (m2rnn_delta_route_string: "step"); other calls go by chunks of steps.
+ *
+ * m2rnn_delta_bwd: gradients of  L = sum y * dy + sum HT * dHT.
+ *   ckpt  what the forward wrote, or NULL: then the states are made again, in the workspace
+ *   dy [B,T,N,V] io    dHT [B,N,K,V] fp32 or NULL (zero)
+ *   dq, dk [B,T,Nqk,K] io (summed over the heads that share one)    dv [B,T,N,V] io
+ *   dg, dbeta [B,T,N] io (bf16 too: the sums behind them are no finer there)
+ *   dH0 [B,N,K,V] fp32, or NULL
+ *   workspace: m2rnn_delta_workspace_bytes(desc, 0 forward | 1 backward with ckpt | 2 without).
+ * Numbers: fp32 io is computed in fp32 throughout.
+ * A NaN or an infinity in the inputs of a step may reach y of up to 63 steps before it (the steps of a chunk
+ * are computed together), and its gradients those of the chunk.
+ * Errors as for the scan; M2RNN_ERR_CHUNK for a chunk that is not 0.
+ */
+size_t m2rnn_delta_ckpt_bytes(const m2rnn_desc *desc);
+size_t m2rnn_delta_workspace_bytes(const m2rnn_desc *desc, int bwd);
+const char *m2rnn_delta_route_string(const m2rnn_desc *desc, int bwd);
+m2rnn_status m2rnn_delta_fwd(const m2rnn_desc *desc, const void *q, const void *k, const void *v, const float *g,
+                             const float *beta, const float *H0, void *y, float *HT, void *ckpt, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+m2rnn_status m2rnn_delta_bwd(const m2rnn_desc *desc, const void *q, const void *k, const void *v, const float *g,
+                             const float *beta, const float *H0, const void *ckpt, const void *dy, const float *dHT,
+                             void *dq, void *dk, void *dv, void *dg, void *dbeta, float *dH0, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
 
 /*
  * m2rnn_fwd_opt for callers that cannot allocate device memory or size a workspace: code

@@ -13,13 +13,18 @@ LIB_PATH = os.path.join(_HERE, "libm2rnn.so")
 
 M2RNN_F32 = 0
 M2RNN_BF16 = 1
+M2RNN_NORM_CENTER = 1
+M2RNN_NORM_SILU = 2
 
 EXPORTS = ("m2rnn_status_string", "m2rnn_default_chunk", "m2rnn_max_chunk",
            "m2rnn_ckpt_bytes", "m2rnn_workspace_bytes", "m2rnn_fwd", "m2rnn_bwd",
            "m2rnn_fwd_opt", "m2rnn_bwd_opt", "m2rnn_fwd_static", "m2rnn_route_string",
            "m2rnn_conv_silu_workspace_bytes", "m2rnn_conv_silu_fwd", "m2rnn_conv_silu_bwd",
            "m2rnn_gated_rmsnorm_workspace_bytes", "m2rnn_gated_rmsnorm_fwd",
-           "m2rnn_gated_rmsnorm_bwd")
+           "m2rnn_gated_rmsnorm_bwd", "m2rnn_conv_silu_window_fwd",
+           "m2rnn_group_norm_workspace_bytes", "m2rnn_group_norm_fwd", "m2rnn_group_norm_bwd",
+           "m2rnn_delta_ckpt_bytes", "m2rnn_delta_workspace_bytes", "m2rnn_delta_route_string",
+           "m2rnn_delta_fwd", "m2rnn_delta_bwd")
 M2RNN_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -93,6 +98,24 @@ def lib():
         L.m2rnn_gated_rmsnorm_fwd.argtypes = [i32] * 4 + [vp] * 3 + [fl] + [vp] * 3
         L.m2rnn_gated_rmsnorm_bwd.restype = ctypes.c_int
         L.m2rnn_gated_rmsnorm_bwd.argtypes = [i32] * 4 + [vp] * 3 + [fl] + [vp] * 6 + [sz, vp]
+        L.m2rnn_conv_silu_window_fwd.restype = ctypes.c_int
+        L.m2rnn_conv_silu_window_fwd.argtypes = [i32] * 4 + [vp] * 7
+        L.m2rnn_group_norm_workspace_bytes.restype = sz
+        L.m2rnn_group_norm_workspace_bytes.argtypes = [i32] * 3
+        L.m2rnn_group_norm_fwd.restype = ctypes.c_int
+        L.m2rnn_group_norm_fwd.argtypes = [i32] * 6 + [vp] * 4 + [fl] + [vp] * 2
+        L.m2rnn_group_norm_bwd.restype = ctypes.c_int
+        L.m2rnn_group_norm_bwd.argtypes = [i32] * 6 + [vp] * 4 + [fl] + [vp] * 6 + [sz, vp]
+        L.m2rnn_delta_ckpt_bytes.restype = sz
+        L.m2rnn_delta_ckpt_bytes.argtypes = [dp]
+        L.m2rnn_delta_workspace_bytes.restype = sz
+        L.m2rnn_delta_workspace_bytes.argtypes = [dp, ctypes.c_int]
+        L.m2rnn_delta_route_string.restype = ctypes.c_char_p
+        L.m2rnn_delta_route_string.argtypes = [dp, ctypes.c_int]
+        L.m2rnn_delta_fwd.restype = ctypes.c_int
+        L.m2rnn_delta_fwd.argtypes = [dp] + [vp] * 10 + [sz, vp]
+        L.m2rnn_delta_bwd.restype = ctypes.c_int
+        L.m2rnn_delta_bwd.argtypes = [dp] + [vp] * 16 + [sz, vp]
         _lib = L
     return _lib
 
@@ -118,6 +141,7 @@ def _call():
                                % (built_for, torch.__version__, again))
         address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         module.init(address(L.m2rnn_fwd_opt), address(L.m2rnn_bwd_opt))
+        module.init_delta(address(L.m2rnn_delta_fwd), address(L.m2rnn_delta_bwd))
         _call_module = module
     return _call_module
 
@@ -276,6 +300,62 @@ def m2rnn_gated_rmsnorm_bwd(y, a, w, eps, s, dout, dy, da, dw, workspace, stream
     return _check(rc, "m2rnn_gated_rmsnorm_bwd", check)
 
 
+def m2rnn_conv_silu_window_fwd(x, w, bias, win, out, win_out, stream=None, check=True):
+    """m2rnn_conv_silu_fwd that starts from the steps in win [B,3,C] (None: zeros) and hands its last three
+    on in win_out (None: not wanted; may be win)."""
+    B, T, C = x.shape
+    rc = lib().m2rnn_conv_silu_window_fwd(B, T, C, _io_code(x), _ptr(x), _ptr(w), _ptr(bias), _ptr(win),
+                                          _ptr(out), _ptr(win_out), stream or 0)
+    return _check(rc, "m2rnn_conv_silu_window_fwd", check)
+
+
+def m2rnn_group_norm_workspace_bytes(B, T, D):
+    return int(lib().m2rnn_group_norm_workspace_bytes(B, T, D))
+
+
+def m2rnn_group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream=None, check=True):
+    """out = n, SiLU(n) (M2RNN_NORM_SILU) or n SiLU(a): n is x [B,T,D], each token's `groups` groups of channels
+    normalised (M2RNN_NORM_CENTER: about their mean), times w [D] plus b [D] (None: 1, 0)."""
+    B, T, D = x.shape
+    rc = lib().m2rnn_group_norm_fwd(B, T, D, groups, _io_code(x), mode, _ptr(x), _ptr(a), _ptr(w), _ptr(b),
+                                    float(eps), _ptr(out), stream or 0)
+    return _check(rc, "m2rnn_group_norm_fwd", check)
+
+
+def m2rnn_group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, stream=None, check=True):
+    B, T, D = x.shape
+    rc = lib().m2rnn_group_norm_bwd(B, T, D, groups, _io_code(x), mode, _ptr(x), _ptr(a), _ptr(w), _ptr(b),
+                                    float(eps), _ptr(dout), _ptr(dx), _ptr(da), _ptr(dw), _ptr(db),
+                                    _ptr(workspace), _nbytes(workspace), stream or 0)
+    return _check(rc, "m2rnn_group_norm_bwd", check)
+
+
+def m2rnn_delta_ckpt_bytes(desc):
+    return int(lib().m2rnn_delta_ckpt_bytes(ctypes.byref(desc)))
+
+
+def m2rnn_delta_workspace_bytes(desc, bwd):
+    return int(lib().m2rnn_delta_workspace_bytes(ctypes.byref(desc), int(bwd)))
+
+
+def m2rnn_delta_route_string(desc, bwd):
+    return lib().m2rnn_delta_route_string(ctypes.byref(desc), int(bwd)).decode()
+
+
+def m2rnn_delta_fwd(desc, q, k, v, g, beta, H0, y, HT, ckpt, workspace, stream=None, check=True):
+    rc = lib().m2rnn_delta_fwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(H0),
+                               _ptr(y), _ptr(HT), _ptr(ckpt), _ptr(workspace), _nbytes(workspace), stream or 0)
+    return _check(rc, "m2rnn_delta_fwd", check)
+
+
+def m2rnn_delta_bwd(desc, q, k, v, g, beta, H0, ckpt, dy, dHT, dq, dk, dv, dg, dbeta, dH0, workspace, stream=None,
+                    check=True):
+    rc = lib().m2rnn_delta_bwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(H0),
+                               _ptr(ckpt), _ptr(dy), _ptr(dHT), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dg),
+                               _ptr(dbeta), _ptr(dH0), _ptr(workspace), _nbytes(workspace), stream or 0)
+    return _check(rc, "m2rnn_delta_bwd", check)
+
+
 # --------------------------------------------------------------------------
 # Buffer plumbing for callers that hold torch tensors: allocates outputs,
 # checkpoints and workspace with torch and calls the raw entry points on
@@ -348,4 +428,50 @@ class Scan:
                               self.dH0, ws, self._stream(), _nbytes(ws), 0.0 if plain else grad_clip)
         if rc != 0:
             raise M2RNNError(rc, "m2rnn_bwd" if plain else "m2rnn_bwd_opt")
+        return out
+
+
+class Delta:
+    """Owns the outputs / checkpoint / workspace buffers of one problem shape of the gated delta rule."""
+
+    def __init__(self, B, T, N, K, V, io, Nqk=None, backward=True, device="cuda"):
+        import torch
+        self.torch = torch
+        self._native = _call()
+        self.desc = d = make_desc(B, T, N, K, V, M2RNN_BF16 if io in ("bf16", M2RNN_BF16) else M2RNN_F32, Nqk=Nqk)
+        self.io_dtype = torch.bfloat16 if d.io == M2RNN_BF16 else torch.float32
+        new = lambda *shape, dtype=self.io_dtype: torch.empty(shape, dtype=dtype, device=device)
+        self.y, self.HT = new(B, T, N, V), new(B, N, K, V, dtype=torch.float32)
+        self.backward = backward
+        ws = m2rnn_delta_workspace_bytes(d, 0)
+        self.ckpt = None
+        if backward:
+            # (2: also room for the states that bwd(use_ckpt=False) makes again)
+            ws = max(ws, m2rnn_delta_workspace_bytes(d, 2))
+            self.ckpt = new(max(1, m2rnn_delta_ckpt_bytes(d)), dtype=torch.uint8)
+            self.dq, self.dk = new(B, T, d.Nqk, K), new(B, T, d.Nqk, K)
+            self.dv, self.dg, self.dbeta = new(B, T, N, V), new(B, T, N), new(B, T, N)
+            self.dH0 = new(B, N, K, V, dtype=torch.float32)
+        self.workspace = new(max(ws, 256), dtype=torch.uint8)
+
+    _stream = Scan._stream
+
+    def fwd(self, q, k, v, g, beta, H0=None):
+        """q, k [B,T,Nqk,K], v [B,T,N,V]; g [B,T,N] fp32 the log of the gate, beta [B,T,N] fp32.  H0 may be the HT of
+        the call before (a decode loop): the state is then carried in place."""
+        ws = self.workspace
+        rc = self._native.delta_fwd(ctypes.addressof(self.desc), q, k, v, g, beta, H0, self.y, self.HT, self.ckpt, ws,
+                                    self._stream(), _nbytes(ws))
+        if rc != 0:
+            raise M2RNNError(rc, "m2rnn_delta_fwd")
+        return self.y, self.HT
+
+    def bwd(self, q, k, v, g, beta, H0, dy, dHT=None, use_ckpt=True):
+        """dq, dk, dv, dg, dbeta (io dtype) and dH0 (fp32)."""
+        out = (self.dq, self.dk, self.dv, self.dg, self.dbeta, self.dH0)
+        ws = self.workspace
+        rc = self._native.delta_bwd(ctypes.addressof(self.desc), q, k, v, g, beta, H0, self.ckpt if use_ckpt else None,
+                                    dy, dHT, *out, ws, self._stream(), _nbytes(ws))
+        if rc != 0:
+            raise M2RNNError(rc, "m2rnn_delta_bwd")
         return out

@@ -405,6 +405,20 @@ m2rnn_status m2rnn_conv_silu_fwd(int32_t B, int32_t T, int32_t C, int32_t io, co
              ? M2RNN_OK : M2RNN_ERR_HIP;
 }
 
+m2rnn_status m2rnn_conv_silu_window_fwd(int32_t B, int32_t T, int32_t C, int32_t io, const void *x,
+                                        const void *w, const void *bias, const void *win, void *out,
+                                        void *win_out, void *hip_stream) {
+  m2rnn_status st = check_block(B, T, C, io);
+  if (st != M2RNN_OK) return st;
+  const bool any = (size_t)B * T > 0;
+  if (!w || (any && (!x || !out))) return M2RNN_ERR_NULL;
+  const void *ptrs[] = {x, w, bias, win, out, win_out};
+  for (const void *p : ptrs)
+    if (misaligned(p)) return M2RNN_ERR_ALIGN;
+  return conv_silu_window_fwd(B, T, C, io, x, w, bias, win, out, win_out, (hipStream_t)hip_stream) == hipSuccess
+             ? M2RNN_OK : M2RNN_ERR_HIP;
+}
+
 m2rnn_status m2rnn_conv_silu_bwd(int32_t B, int32_t T, int32_t C, int32_t io, const void *x,
                                  const void *w, const void *bias, const void *dout, void *dx,
                                  float *dw, float *dbias, void *workspace, size_t workspace_bytes,
@@ -460,6 +474,66 @@ m2rnn_status m2rnn_gated_rmsnorm_bwd(int32_t B, int32_t T, int32_t D, int32_t io
   if (workspace_bytes < gated_rmsnorm_scratch_bytes(B, T, D)) return M2RNN_ERR_WORKSPACE;
   return gated_rmsnorm_bwd(B, T, D, io, y, a, w, eps, s, dout, dy, da, dw, (float *)workspace,
                            (hipStream_t)hip_stream) == hipSuccess ? M2RNN_OK : M2RNN_ERR_HIP;
+}
+
+// ---- group norm with an activation ----
+
+static m2rnn_status check_group_norm(int32_t B, int32_t T, int32_t D, int32_t groups, int32_t io, int32_t mode,
+                                     float eps, const void *a) {
+  const m2rnn_status st = check_block(B, T, D, io);
+  if (st != M2RNN_OK) return st;
+  if (groups < 1 || D % groups != 0 || (D / groups) % 8 != 0 || D / groups > group_norm_max_group() || !(eps >= 0.f))
+    return M2RNN_ERR_SHAPE;
+  if ((mode & ~(M2RNN_NORM_CENTER | M2RNN_NORM_SILU)) != 0 || ((mode & M2RNN_NORM_SILU) && a)) return M2RNN_ERR_SHAPE;
+  return M2RNN_OK;
+}
+
+static GroupNormArgs group_norm_args(int32_t B, int32_t T, int32_t D, int32_t groups, int32_t io, int32_t mode,
+                                     float eps, const void *x, const void *a, const void *w, const void *b) {
+  GroupNormArgs g = {};
+  g.B = B; g.T = T; g.D = D; g.G = groups; g.io = io; g.eps = eps;
+  g.center = (mode & M2RNN_NORM_CENTER) != 0;
+  g.silu = (mode & M2RNN_NORM_SILU) != 0;
+  g.x = x; g.a = a; g.w = w; g.b = b;
+  return g;
+}
+
+size_t m2rnn_group_norm_workspace_bytes(int32_t B, int32_t T, int32_t D) {
+  return check_block(B, T, D, M2RNN_F32) == M2RNN_OK ? group_norm_scratch_bytes(B, T, D) : 0;
+}
+
+m2rnn_status m2rnn_group_norm_fwd(int32_t B, int32_t T, int32_t D, int32_t groups, int32_t io, int32_t mode,
+                                  const void *x, const void *a, const void *w, const void *b, float eps, void *out,
+                                  void *hip_stream) {
+  const m2rnn_status st = check_group_norm(B, T, D, groups, io, mode, eps, a);
+  if (st != M2RNN_OK) return st;
+  if ((size_t)B * T > 0 && (!x || !out)) return M2RNN_ERR_NULL;
+  const void *ptrs[] = {x, a, w, b, out};
+  for (const void *p : ptrs)
+    if (misaligned(p)) return M2RNN_ERR_ALIGN;
+  GroupNormArgs g = group_norm_args(B, T, D, groups, io, mode, eps, x, a, w, b);
+  g.out = out;
+  return group_norm_fwd(g, (hipStream_t)hip_stream) == hipSuccess ? M2RNN_OK : M2RNN_ERR_HIP;
+}
+
+m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t groups, int32_t io, int32_t mode,
+                                  const void *x, const void *a, const void *w, const void *b, float eps,
+                                  const void *dout, void *dx, void *da, float *dw, float *db, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream) {
+  const m2rnn_status st = check_group_norm(B, T, D, groups, io, mode, eps, a);
+  if (st != M2RNN_OK) return st;
+  if ((size_t)B * T > 0 && (!x || !dout || !dx || (a && !da))) return M2RNN_ERR_NULL;
+  const void *ptrs[] = {x, a, w, b, dout, dx, da, dw, db, workspace};
+  for (const void *p : ptrs)
+    if (misaligned(p)) return M2RNN_ERR_ALIGN;
+  GroupNormArgs g = group_norm_args(B, T, D, groups, io, mode, eps, x, a, w, b);
+  if (dw || db) {
+    if (!workspace) return M2RNN_ERR_NULL;
+    if (workspace_bytes < group_norm_scratch_bytes(B, T, D)) return M2RNN_ERR_WORKSPACE;
+    g.part = (float *)workspace;
+  }
+  g.dout = dout; g.dx = dx; g.da = da; g.dw = dw; g.db = db;
+  return group_norm_bwd(g, (hipStream_t)hip_stream) == hipSuccess ? M2RNN_OK : M2RNN_ERR_HIP;
 }
 
 }  // extern "C"

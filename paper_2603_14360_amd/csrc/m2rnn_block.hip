@@ -11,19 +11,12 @@
 // that stages the same q, k, v rows would add exactly the instructions that bind it.  Here
 // each tensor makes one trip through HBM: x -> out, and (y, a) -> out.
 // Sums over tokens (dw, dbias) are two-stage and ordered: bit-reproducible, no atomics.
-#include "m2rnn_io.hpp"
-#include "m2rnn_kernels.hpp"
-#include "m2rnn_mfma_common.hpp"
+#include "m2rnn_block.hpp"
 
 #include <algorithm>
 
 namespace m2rnn {
 namespace {
-
-// 1 / (1 + e^-u) on the hardware's exp2 and reciprocal (1 ulp each; e^-u = inf gives 0)
-__device__ __forceinline__ float sigmoidf_(float u) {
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u));
-}
 
 // ------------------------------------------------------------------ conv1d(4) + SiLU
 constexpr int kTaps = 4;
@@ -72,10 +65,14 @@ inline ConvPlan conv_plan(int B, int T, int C, int most_rows) {
   return p;
 }
 
-template <typename IO>
+// WIN: the steps in front of the first are the rows of `win` [B,3,C] and not zeros, and the last three go
+// to `win_out`, both by the item that starts a batch row: it has read all of `win` when it writes, and no other
+// item reads it, so the two may be one buffer.
+template <typename IO, bool WIN>
 __global__ void __launch_bounds__(kThreads)
     conv_silu_fwd_kernel(const void *__restrict__ x, const void *__restrict__ w,
-                         const void *__restrict__ bias, void *__restrict__ out, int B, int T, int C, ConvPlan p) {
+                         const void *__restrict__ bias, void *__restrict__ out, int B, int T, int C, ConvPlan p,
+                         const void *win_in, void *win_out) {
   constexpr int BLK = 8;  // steps whose loads are issued together
   const int wl = threadIdx.x / p.cw, cl = threadIdx.x - wl * p.cw;
   const int bx = blockIdx.x % p.gx, rgi = blockIdx.x / p.gx;
@@ -93,9 +90,23 @@ __global__ void __launch_bounds__(kThreads)
     for (int j = 0; j < kTaps - 1; ++j) {
       const int ts = t0 - (kTaps - 1) + j;
       if (ts >= 0) Vec4<IO>::widen(Vec4<IO>::load_raw(x, base + (size_t)ts * C), win[j]);
+      else if (WIN && win_in)
+        Vec4<IO>::widen(Vec4<IO>::load_raw(win_in, ((size_t)b * (kTaps - 1) + j) * C + c0), win[j]);
       else
 #pragma unroll
         for (int i = 0; i < 4; ++i) win[j][i] = 0.f;
+    }
+    if (WIN && win_out && seg == 0) {
+#pragma unroll
+      for (int j = 0; j < kTaps - 1; ++j) {
+        const int ts = T - (kTaps - 1) + j;  // (below zero: row T + j of the window that came in)
+        float last[4];
+        if (ts >= 0) Vec4<IO>::widen(Vec4<IO>::load_raw(x, base + (size_t)ts * C), last);
+        else
+#pragma unroll
+          for (int i = 0; i < 4; ++i) last[i] = T + j == 0 ? win[0][i] : T + j == 1 ? win[1][i] : win[2][i];
+        Vec4<IO>::store(win_out, ((size_t)b * (kTaps - 1) + j) * C + c0, last);
+      }
     }
     for (int tb = t0; tb < t1; tb += BLK) {
       typename Vec4<IO>::Raw raw[BLK];
@@ -238,14 +249,6 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
 }
 
-// Ordered sum of R partial rows of E floats.  A workgroup adds up to 32 columns with 32 walkers
-// (rows wl, wl + 32, ..., four loads in flight) and the walkers in LDS.  Up to kDirectRows rows
-// that is all; more are first added in groups of about kDirectRows / 4 (blockIdx.y) into rows
-// of `lvl` (kSumGroups rows behind the partials).  What bounds it is the chain of dependent
-// loads: 128 rows of 7360 took two launches, some 13 us, with one column per thread; 4.7 us now.
-constexpr int kSumGroups = 32;
-constexpr int kDirectRows = 512;
-
 // column e of a plain [D] result, and of the convolution's [C][4 taps, bias]
 struct PlainOut {
   float *out;
@@ -259,31 +262,6 @@ struct ConvOut {
     else if (dbias) dbias[c] = s;
   }
 };
-template <typename Out>
-__global__ void __launch_bounds__(1024)
-    ordered_sum_kernel(const float *__restrict__ part, float *__restrict__ lvl, Out out, int E, int R) {
-  const int e = blockIdx.x * 32 + (threadIdx.x & 31), per = (R + gridDim.y - 1) / gridDim.y;
-  const int r0 = blockIdx.y * per, r1 = r0 + per < R ? r0 + per : R;
-  const float t = column_sum(part, E, e, r0, r1);
-  if (threadIdx.x < 32 && e < E) {
-    if (gridDim.y > 1) lvl[(size_t)blockIdx.y * E + e] = t;
-    else out.put(e, t);
-  }
-}
-template <typename Out>
-hipError_t ordered_sum(const float *part, float *lvl, const Out &out, int E, int R, hipStream_t s) {
-  const int bx = (E + 31) / 32;
-  if (R > kDirectRows) {
-    const int want = (R + kDirectRows / 4 - 1) / (kDirectRows / 4), G = want < kSumGroups ? want : kSumGroups;
-    hipLaunchKernelGGL(ordered_sum_kernel<Out>, dim3(bx, G), dim3(1024), 0, s, part, lvl, out, E, R);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    part = lvl;
-    R = G;
-  }
-  hipLaunchKernelGGL(ordered_sum_kernel<Out>, dim3(bx, 1), dim3(1024), 0, s, part, lvl, out, E, R);
-  return hipGetLastError();
-}
 
 // ------------------------------------------------------------------ gated RMSNorm
 __device__ __forceinline__ float wave_sum(float v) {
@@ -479,14 +457,29 @@ static hipError_t conv_fwd_t(int B, int T, int C, const void *x, const void *w, 
                              void *out, hipStream_t s) {
   if ((size_t)B * T == 0) return hipSuccess;
   const ConvPlan p = conv_plan(B, T, C, 16384);
-  hipLaunchKernelGGL((conv_silu_fwd_kernel<IO>), dim3((unsigned)(p.gx * p.rg)), dim3(kThreads), 0, s, x, w, bias,
-                     out, B, T, C, p);
+  hipLaunchKernelGGL((conv_silu_fwd_kernel<IO, false>), dim3((unsigned)(p.gx * p.rg)), dim3(kThreads), 0, s, x, w,
+                     bias, out, B, T, C, p, nullptr, nullptr);
+  return hipGetLastError();
+}
+template <typename IO>
+static hipError_t conv_window_t(int B, int T, int C, const void *x, const void *w, const void *bias,
+                                const void *win, void *out, void *win_out, hipStream_t s) {
+  if (B == 0) return hipSuccess;
+  const ConvPlan p = conv_plan(B, std::max(T, 1), C, 16384);  // (no steps: the window alone is handed on)
+  hipLaunchKernelGGL((conv_silu_fwd_kernel<IO, true>), dim3((unsigned)(p.gx * p.rg)), dim3(kThreads), 0, s, x, w,
+                     bias, out, B, T, C, p, win, win_out);
   return hipGetLastError();
 }
 hipError_t conv_silu_fwd(int B, int T, int C, int io, const void *x, const void *w, const void *bias,
                          void *out, hipStream_t s) {
   return io == 0 ? conv_fwd_t<float>(B, T, C, x, w, bias, out, s)
                  : conv_fwd_t<__hip_bfloat16>(B, T, C, x, w, bias, out, s);
+}
+
+hipError_t conv_silu_window_fwd(int B, int T, int C, int io, const void *x, const void *w, const void *bias,
+                                const void *win, void *out, void *win_out, hipStream_t s) {
+  return io == 0 ? conv_window_t<float>(B, T, C, x, w, bias, win, out, win_out, s)
+                 : conv_window_t<__hip_bfloat16>(B, T, C, x, w, bias, win, out, win_out, s);
 }
 
 template <typename IO>

@@ -156,6 +156,9 @@ hipError_t conv_silu_fwd(int B, int T, int C, int io, const void *x, const void 
 hipError_t conv_silu_bwd(int B, int T, int C, int io, const void *x, const void *w, const void *bias,
                          const void *dout, void *dx, float *dw, float *dbias, float *part,
                          hipStream_t s);
+// the forward from the three steps in `win` on; the last three to `win_out` (null: zeros, not wanted)
+hipError_t conv_silu_window_fwd(int B, int T, int C, int io, const void *x, const void *w, const void *bias,
+                                const void *win, void *out, void *win_out, hipStream_t s);
 size_t gated_rmsnorm_scratch_bytes(int B, int T, int D);
 int gated_rmsnorm_max_features();
 hipError_t gated_rmsnorm_fwd(int B, int T, int D, int io, const void *y, const void *a, const void *w,
@@ -163,6 +166,23 @@ hipError_t gated_rmsnorm_fwd(int B, int T, int D, int io, const void *y, const v
 hipError_t gated_rmsnorm_bwd(int B, int T, int D, int io, const void *y, const void *a, const void *w,
                              float eps, const float *s_in, const void *dout, void *dy, void *da,
                              float *dw, float *part, hipStream_t s);
+
+// ---- group norm of a token's channels with an activation ----
+struct GroupNormArgs {
+  int B, T, D, G, io;
+  bool center, silu;
+  float eps;
+  const void *x, *a, *w, *b;  // a, w, b may be null
+  void *out;
+  const void *dout;
+  void *dx, *da;
+  float *dw, *db;  // may be null
+  float *part;     // scratch of group_norm_scratch_bytes() (backward with dw or db)
+};
+size_t group_norm_scratch_bytes(int B, int T, int D);
+int group_norm_max_group();
+hipError_t group_norm_fwd(const GroupNormArgs &a, hipStream_t s);
+hipError_t group_norm_bwd(const GroupNormArgs &a, hipStream_t s);
 
 // ---- single-step decode (bf16 io, V <= 64, T == 1): one launch, no staging, no workspace ----
 bool decode_supported(int K, int V);

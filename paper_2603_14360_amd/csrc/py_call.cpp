@@ -1,4 +1,4 @@
-// Python module _call: the scan's two entry points of the C ABI called with torch tensors.
+// Python module _call: the entry points of the C ABI that Scan and Delta call, called with torch tensors.
 //
 // A decode step is one kernel of some 4 us, and handing its sixteen arguments over through ctypes took
 // 2.5 us of host time (on a slower host 6), beside a launch of 3.5.  Here the addresses are taken from the
@@ -13,6 +13,8 @@ namespace {
 
 decltype(&m2rnn_fwd_opt) fwd_opt = nullptr;
 decltype(&m2rnn_bwd_opt) bwd_opt = nullptr;
+decltype(&m2rnn_delta_fwd) delta_fwd = nullptr;
+decltype(&m2rnn_delta_bwd) delta_bwd = nullptr;
 
 // None -> NULL, an int as it is, a tensor -> its address, anything else -> what its data_ptr() says (a
 // subclass of the tensor may have its own); false with a Python error set otherwise
@@ -119,7 +121,51 @@ PyObject *bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
+PyObject *init_delta(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  void *p[2];
+  if (!arity(n, 2) || !addresses(args, p)) return nullptr;
+  if (!p[0] || !p[1]) {
+    PyErr_SetString(PyExc_ValueError, "an entry point is NULL");
+    return nullptr;
+  }
+  delta_fwd = (decltype(delta_fwd))p[0];
+  delta_bwd = (decltype(delta_bwd))p[1];
+  Py_RETURN_NONE;
+}
+
+// delta_fwd(desc, q, k, v, g, beta, H0, y, HT, ckpt, workspace, stream, bytes) -> status
+PyObject *call_delta_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  void *p[12];
+  if (!ready((const void *)delta_fwd) || !arity(n, 13) || !addresses(args, p)) return nullptr;
+  const size_t bytes = PyLong_AsSize_t(args[12]);
+  if (bytes == (size_t)-1 && PyErr_Occurred()) return nullptr;
+  m2rnn_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = delta_fwd((const m2rnn_desc *)p[0], p[1], p[2], p[3], (const float *)p[4], (const float *)p[5],
+                 (const float *)p[6], p[7], (float *)p[8], p[9], p[10], bytes, p[11]);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// delta_bwd(desc, q, k, v, g, beta, H0, ckpt, dy, dHT, dq, dk, dv, dg, dbeta, dH0, workspace, stream, bytes) -> status
+PyObject *call_delta_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  void *p[18];
+  if (!ready((const void *)delta_bwd) || !arity(n, 19) || !addresses(args, p)) return nullptr;
+  const size_t bytes = PyLong_AsSize_t(args[18]);
+  if (bytes == (size_t)-1 && PyErr_Occurred()) return nullptr;
+  m2rnn_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = delta_bwd((const m2rnn_desc *)p[0], p[1], p[2], p[3], (const float *)p[4], (const float *)p[5],
+                 (const float *)p[6], p[7], p[8], (const float *)p[9], p[10], p[11], p[12], p[13], p[14], (float *)p[15],
+                 p[16], bytes, p[17]);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
 PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)(void))init, METH_FASTCALL, nullptr},
+                         {"init_delta", (PyCFunction)(void (*)(void))init_delta, METH_FASTCALL, nullptr},
+                         {"delta_fwd", (PyCFunction)(void (*)(void))call_delta_fwd, METH_FASTCALL, nullptr},
+                         {"delta_bwd", (PyCFunction)(void (*)(void))call_delta_bwd, METH_FASTCALL, nullptr},
                          {"fwd", (PyCFunction)(void (*)(void))fwd, METH_FASTCALL, nullptr},
                          {"bwd", (PyCFunction)(void (*)(void))bwd, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

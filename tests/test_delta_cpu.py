@@ -1,0 +1,129 @@
+"""CPU-only: sizes, routes and refusals of the gated delta rule, the group norm and the windowed convolution.
+Nothing is launched: every call here is refused, or has nothing to do."""
+import ctypes
+
+import pytest
+
+from paper_2603_14360_amd import binding as mb
+
+
+class Buf:
+    def __init__(self, addr=0x100000, nbytes=1 << 40):
+        self.addr, self.nbytes = addr, nbytes
+
+    def data_ptr(self):
+        return self.addr
+
+
+A, BIG = 0x1000, Buf()
+
+
+def desc(**kw):
+    return mb.make_desc(**dict(dict(B=2, T=70, N=4, K=32, V=32, io=mb.M2RNN_BF16), **kw))
+
+
+def fwd(d, q=A, k=A, v=A, g=A, beta=A, H0=None, y=A, HT=A, ckpt=None, ws=BIG):
+    return mb.m2rnn_delta_fwd(d, q, k, v, g, beta, H0, y, HT, ckpt, ws, check=False)
+
+
+def bwd(d, q=A, k=A, v=A, g=A, beta=A, H0=None, ckpt=A, dy=A, dHT=None, dq=A, dk=A, dv=A, dg=A, dbeta=A, dH0=A, ws=BIG):
+    return mb.m2rnn_delta_bwd(d, q, k, v, g, beta, H0, ckpt, dy, dHT, dq, dk, dv, dg, dbeta, dH0, ws, check=False)
+
+
+BAD = [(dict(K=24), 2), (dict(K=256), 2), (dict(V=48), 2), (dict(V=512), 2), (dict(N=0), 2), (dict(Nqk=3), 2),
+       (dict(Nqk=0), 2), (dict(B=-1), 2), (dict(T=-1), 2), (dict(io=5), 3), (dict(flags=1), 2), (dict(chunk=16), 7),
+       (dict(B=1 << 30, N=1 << 20), 2), (dict(B=1 << 20, N=64, T=1 << 20), 2)]
+
+
+@pytest.mark.parametrize("kw,code", BAD)
+def test_bad_descriptors_are_refused(kw, code):
+    d = desc(**kw)
+    assert fwd(d) == code and bwd(d) == code
+    assert mb.m2rnn_delta_ckpt_bytes(d) == mb.m2rnn_delta_workspace_bytes(d, 0) == mb.m2rnn_delta_workspace_bytes(d, 2) == 0
+    assert mb.m2rnn_delta_route_string(d, 0) == "invalid descriptor"
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "g", "beta", "y"])
+def test_forward_needs_its_tensors(name):
+    assert fwd(desc(), **{name: None}) == 1
+    assert fwd(desc(), **{name: A + 8}) == 4
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "g", "beta", "dy", "dq", "dk", "dv", "dg", "dbeta"])
+def test_backward_needs_its_tensors(name):
+    assert bwd(desc(), **{name: None}) == 1
+    assert bwd(desc(), **{name: A + 4}) == 4
+
+
+@pytest.mark.parametrize("name", ["H0", "HT", "ckpt"])
+def test_optional_tensors_are_aligned(name):
+    assert fwd(desc(), **{name: A + 4}) == 4
+
+
+@pytest.mark.parametrize("name", ["H0", "dHT", "dH0", "ckpt"])
+def test_optional_tensors_of_the_backward_are_aligned(name):
+    assert bwd(desc(), **{name: A + 4}) == 4
+
+
+@pytest.mark.parametrize("io", [mb.M2RNN_F32, mb.M2RNN_BF16])
+@pytest.mark.parametrize("Nqk", [4, 2])
+@pytest.mark.parametrize("T", [1, 9, 64, 1000])
+def test_workspace(io, Nqk, T):
+    d = desc(T=T, Nqk=Nqk, io=io)
+    for ckpt, bwd_mode in ((A, 1), (None, 2)):
+        need = mb.m2rnn_delta_workspace_bytes(d, bwd_mode)
+        assert need > 0
+        assert bwd(d, ckpt=ckpt, ws=Buf(nbytes=need - 1)) == 5 and bwd(d, ckpt=ckpt, ws=None) == 1
+    assert mb.m2rnn_delta_workspace_bytes(d, 2) == mb.m2rnn_delta_workspace_bytes(d, 1) + mb.m2rnn_delta_ckpt_bytes(d)
+    need = mb.m2rnn_delta_workspace_bytes(d, 0)
+    assert fwd(d, ckpt=A, ws=Buf(nbytes=need - 1)) == 5 and fwd(d, ckpt=A, ws=None) == 1
+    if mb.m2rnn_delta_route_string(d, 0) != "step":
+        assert fwd(d, ws=Buf(nbytes=need - 1)) == 5 and fwd(d, ws=None) == 1
+
+
+def test_an_empty_batch_has_nothing_to_do():
+    d = desc(B=0)
+    assert fwd(d, q=None, k=None, v=None, g=None, beta=None, y=None, HT=None, ws=None) == 0
+    assert bwd(d, *[None] * 16) == 0
+
+
+def test_one_token_runs_the_recurrence():
+    assert mb.m2rnn_delta_route_string(desc(T=1), 0) == "step"
+    assert mb.m2rnn_delta_route_string(desc(T=1), 1) != "step"
+    assert mb.m2rnn_delta_route_string(desc(T=4096), 0) != "step"
+
+
+def test_group_norm_refusals():
+    L, p = mb.lib(), ctypes.c_void_p(A)
+    odd = ctypes.c_void_p(A + 4)
+
+    def f(B=2, T=5, D=64, G=4, io=1, mode=0, x=p, a=None, w=p, b=p, eps=1e-5, out=p):
+        return L.m2rnn_group_norm_fwd(B, T, D, G, io, mode, x, a, w, b, eps, out, None)
+
+    def r(B=2, T=5, D=64, G=4, io=1, mode=0, x=p, a=None, w=p, b=p, eps=1e-5, dout=p, dx=p, da=None, dw=p, db=p, ws=p,
+          n=1 << 30):
+        return L.m2rnn_group_norm_bwd(B, T, D, G, io, mode, x, a, w, b, eps, dout, dx, da, dw, db, ws, n, None)
+
+    for call in (f, r):
+        for kw in (dict(D=60), dict(G=0), dict(G=5), dict(G=16), dict(D=2048, G=1), dict(eps=-1.0), dict(eps=float("nan")),
+                   dict(mode=4), dict(mode=-1), dict(mode=mb.M2RNN_NORM_SILU, a=p), dict(B=-1), dict(T=-1)):
+            assert call(**kw) == 2, kw
+        assert call(io=2) == 3
+        assert call(x=None) == 1 and call(x=odd) == 4 and call(w=odd) == 4 and call(b=odd) == 4
+    assert f(out=None) == 1 and f(out=odd) == 4 and f(a=odd) == 4
+    assert r(dout=None) == 1 and r(dx=None) == 1 and r(a=p) == 1 and r(a=p, da=odd) == 4
+    assert r(ws=None) == 1 and r(n=16) == 5 and r(dw=odd) == 4
+    assert mb.m2rnn_group_norm_workspace_bytes(2, 5, 60) == 0 < mb.m2rnn_group_norm_workspace_bytes(2, 5, 64)
+
+
+def test_window_refusals():
+    L, p, odd = mb.lib(), ctypes.c_void_p(A), ctypes.c_void_p(A + 2)
+
+    def f(B=2, T=5, C=64, io=1, x=p, w=p, bias=None, win=p, out=p, win_out=p):
+        return L.m2rnn_conv_silu_window_fwd(B, T, C, io, x, w, bias, win, out, win_out, None)
+
+    assert f(C=12) == 2 and f(T=-1) == 2 and f(io=3) == 3
+    assert f(x=None) == f(w=None) == f(out=None) == 1
+    for n in ("x", "w", "bias", "win", "out", "win_out"):
+        assert f(**{n: odd}) == 4
+    assert f(B=0) == 0
