@@ -53,12 +53,19 @@ struct DeltaLayout {
   size_t mats;    // T and P of every chunk
   size_t states;  // one state per chunk
   size_t rows;    // U or Z of every step
+  size_t scales;  // powers of two of the gradients (0: none)
   size_t heads;   // dq or dk of every head in fp32 (0 where no heads share q, k)
 };
 
 DeltaLayout delta_f32_layout(const DeltaArgs &a);
 hipError_t delta_f32_fwd(const DeltaArgs &a, hipStream_t s);
 hipError_t delta_f32_bwd(const DeltaArgs &a, hipStream_t s);
+
+// bf16 io with K, V >= 32: chunks of 64 on the fp16 matrix instructions
+bool delta_half_serves(int K, int V, int io);
+DeltaLayout delta_half_layout(const DeltaArgs &a);
+hipError_t delta_half_fwd(const DeltaArgs &a, hipStream_t s);
+hipError_t delta_half_bwd(const DeltaArgs &a, hipStream_t s);
 
 // The recurrence step by step, the state in registers: serving, and segments of a few steps.
 bool delta_step_serves(int T);

@@ -28,14 +28,15 @@ DeltaArgs args_of(const m2rnn_desc *d) {
   a.write_y = 1;
   return a;
 }
-DeltaLayout layout(const DeltaArgs &a) { return delta_f32_layout(a); }
-hipError_t run_fwd(const DeltaArgs &a, hipStream_t s) { return delta_f32_fwd(a, s); }
-hipError_t run_bwd(const DeltaArgs &a, hipStream_t s) { return delta_f32_bwd(a, s); }
+bool half(const DeltaArgs &a) { return delta_half_serves(a.K, a.V, a.io); }
+DeltaLayout layout(const DeltaArgs &a) { return half(a) ? delta_half_layout(a) : delta_f32_layout(a); }
+hipError_t run_fwd(const DeltaArgs &a, hipStream_t s) { return half(a) ? delta_half_fwd(a, s) : delta_f32_fwd(a, s); }
+hipError_t run_bwd(const DeltaArgs &a, hipStream_t s) { return half(a) ? delta_half_bwd(a, s) : delta_f32_bwd(a, s); }
 
 size_t ckpt_bytes(const DeltaLayout &l) { return l.states + l.rows; }
 size_t ws_bytes(const DeltaLayout &l, int bwd) {
   const size_t fwd = l.gates + l.mats;
-  return bwd ? fwd + l.states + l.rows + 2 * l.heads + (bwd >= 2 ? ckpt_bytes(l) : 0) : fwd;
+  return bwd ? fwd + l.states + l.rows + l.scales + 2 * l.heads + (bwd >= 2 ? ckpt_bytes(l) : 0) : fwd;
 }
 bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }
 
@@ -54,7 +55,7 @@ size_t m2rnn_delta_workspace_bytes(const m2rnn_desc *desc, int bwd) {
 const char *m2rnn_delta_route_string(const m2rnn_desc *desc, int bwd) {
   if (check(desc) != M2RNN_OK) return "invalid descriptor";
   if (!bwd && delta_step_serves(desc->T)) return "step";
-  return "chunk32<f32>";
+  return half(args_of(desc)) ? "chunk64<half>" : "chunk32<f32>";
 }
 
 m2rnn_status m2rnn_delta_fwd(const m2rnn_desc *desc, const void *q, const void *k, const void *v, const float *g,

@@ -1,0 +1,1046 @@
+// Gated delta rule of bf16 io, chunks of 64 steps on the 16x16x32 matrix instructions.  The lines of the rule by
+// chunks stand in m2rnn_delta.hpp.
+//
+//   delta_half_prep_kernel   one workgroup per chunk: gates, T and P             -> workspace
+//   delta_half_fwd_kernel    one workgroup per state and VB columns of V, chunks in order -> y, HT, (H, U)
+//   delta_half_bwd_kernel    the same, backwards                                  -> dv, dH0, dH and Z
+//   delta_half_grad_kernel   one workgroup per chunk                              -> dq, dk, dg, dbeta
+//
+// Operands.  q, k, v, dy are bf16 and exact as fp16 (magnitudes from 2^-17 to 2^15).  Everything that reaches a
+// state enters its product as an fp16 pair hi + lo of 22 bits, so that states and their gradients, which are
+// fp32, are as good as that; what only reaches a bf16 result is one fp16 value of 11 bits.  T is formed in fp32.
+// Gradients may have any magnitude: a chunk's are brought near one by a power of two first.
+//
+// Layout.  Products are D = A B^T with rows contiguous along the contraction: a lane reads eight elements of row
+// (lane % 16) at 8 (lane / 16), and holds rows 4 (lane / 16) .. + 3 of column lane % 16 of D.  What one kernel
+// hands to another (T, P, H, U, dH, Z) is stored as the operands that the reader needs, 16 bytes a lane, 1 KB
+// an operand: no reader goes through LDS for it.
+#include "m2rnn_delta.hpp"
+
+namespace m2rnn {
+namespace {
+
+constexpr int C = 64;
+constexpr int LC = C + 8;       // halfs per row of an LDS array with a chunk's steps side by side
+constexpr int kGates = 5 * C;   // floats per chunk: e^G, e^{G_C - G}, G / ln 2 as hi, lo, beta
+// (Backward: e^G over om = 2^floor(G_0 / ln 2).  e^G goes into fp16 operands there, all of it can be as small as
+// the first step's gate, and the gradient of the state in front is then as small: om is put back in fp32.)
+__device__ __forceinline__ float gate_unit(float hi0) { return exp2_(floorf(hi0)); }
+
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 half_t;
+
+__device__ __forceinline__ f4_t mfma_bf16(u4_t a, u4_t b, f4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8_t, a), __builtin_bit_cast(b8_t, b), c, 0, 0, 0);
+}
+// two floats, rounded to nearest even, as fp16
+__device__ __forceinline__ uint32_t pack2_h(float a, float b) {
+  typedef float f2_t __attribute__((ext_vector_type(2)));
+  const f2_t x = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, h2_t));
+}
+__device__ __forceinline__ u2_t pack4_h(f4_t x) { return u2_t{pack2_h(x[0], x[1]), pack2_h(x[2], x[3])}; }
+// eight bf16 values as fp16
+__device__ __forceinline__ h8_t bf16_to_h8(u4_t w) {
+  u4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = w[i];
+    r[i] = pack2_h(__builtin_bit_cast(float, x << 16), __builtin_bit_cast(float, x & 0xFFFF0000u));
+  }
+  return __builtin_bit_cast(h8_t, r);
+}
+// four floats as fp16 hi and lo parts
+struct Pair4 {
+  u2_t hi, lo;
+};
+__device__ __forceinline__ Pair4 split4(f4_t x) {
+  const u2_t a = split2_hi_lo(x[0], x[1]), b = split2_hi_lo(x[2], x[3]);
+  return Pair4{u2_t{a.x, b.x}, u2_t{a.y, b.y}};
+}
+__device__ __forceinline__ h8_t ld8(const half_t *p) { return *(const h8_t *)p; }
+__device__ __forceinline__ h8_t tr8(const half_t *p0, const half_t *p1) {
+  const h4_t a = lds_ld_tr((const lchar *)p0, 0), b = lds_ld_tr((const lchar *)p1, 0);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// The operand whose 16 rows are columns c0 .. c0 + 15 of an LDS array, contracted over its rows r0 .. r0 + 31
+__device__ __forceinline__ h8_t ld8_tr(const half_t *base, int ld, int r0, int c0) {
+  const int lane = threadIdx.x & 63, d = lane & 15, g = lane >> 4;
+  const half_t *p = base + (r0 + 8 * g + (d >> 2)) * ld + c0 + 4 * (d & 3);
+  return tr8(p, p + 4 * ld);
+}
+
+// ------------------------------------------------------------------ gates, T, P of one chunk
+// T and P of a chunk: [row tile 4][32 columns 2][hi, lo][lane][8].  BWD: of their transposes.
+constexpr size_t kMat = 4 * 2 * 2 * 64 * 8;  // halfs
+__device__ __forceinline__ size_t mat_at(int tile, int kb, int part) { return (size_t)(((tile * 2 + kb) * 2 + part) * 64) * 8; }
+
+__device__ __forceinline__ f4_t mma_f32(const float *a, const float *b, f4_t c) {
+  const f4_t x = *(const f4_t *)a, y = *(const f4_t *)b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+  return c;
+}
+
+// The inverse of I + A by blocks of 16: the diagonal blocks row by row, then
+//     [ T0 0 ; -T1 A10 T0  T1 ]   for the two pairs of neighbours, and the same with blocks of 32,
+// whose products run on the fp32 matrix instructions.
+template <bool BWD>
+__global__ void __launch_bounds__(256) delta_half_prep_kernel(DeltaArgs a, int chunks, float *__restrict__ gates,
+                                                              half_t *__restrict__ mats) {
+  constexpr int LA = C + 4;
+  __shared__ __align__(16) float As[C][LA], Ts[C][LA], Tt[C][LA], Xt[C / 2][C / 2 + 4];
+  __shared__ __align__(16) half_t Ps[BWD ? 2 : 1][C][LC];
+  __shared__ float hi[C], lo[C], be[C];
+  const int unit = blockIdx.x / chunks, ch = blockIdx.x - unit * chunks;
+  const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
+  const int t0 = ch * C, lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int d = lane & 15, g4 = lane >> 4;
+  if (wv == 0) {
+    const bool in = t0 + lane < a.T;
+    const size_t e = ((size_t)b * a.T + (in ? t0 + lane : 0)) * a.N + n;
+    const float beta = in ? a.beta[e] : 0.f;
+    const GateSum G = gate_sum(in ? a.g[e] : 0.f);
+    const float ghi = __shfl(G.hi, C - 1, 64), glo = __shfl(G.lo, C - 1, 64);
+    hi[lane] = G.hi;
+    lo[lane] = G.lo;
+    be[lane] = beta;
+    float *gt = gates + (size_t)blockIdx.x * kGates;
+    gt[lane] = BWD ? exp2_((G.hi - floorf(__shfl(G.hi, 0, 64))) + G.lo) : exp2_(G.hi) * exp2_(G.lo);
+    gt[C + lane] = exp2_((ghi - G.hi) + (glo - G.lo));
+    gt[2 * C + lane] = G.hi;
+    gt[3 * C + lane] = G.lo;
+    gt[4 * C + lane] = beta;
+  }
+  __syncthreads();
+  const size_t row = (size_t)a.Nqk * a.K, base = (size_t)b * a.T * row + (size_t)nq * a.K + 8 * g4;
+  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k;
+  auto at = [&](int tile) { return base + (size_t)min(t0 + 16 * tile + d, a.T - 1) * row; };
+  // forward: wave = tile of i, over j <= i, D[j][i];  backward: wave = tile of j, over i >= j, D[i][j]
+  const size_t own = at(wv);
+  for (int o = BWD ? wv : 0; o < (BWD ? 4 : wv + 1); ++o) {
+    const size_t other = at(o);
+    f4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
+    for (int e = 0; e < a.K; e += 32) {
+      const u4_t ko = *(const u4_t *)(k + other + e), kw = *(const u4_t *)(k + own + e);
+      kk = mfma_bf16(ko, kw, kk);
+      if (BWD) qk = mfma_bf16(*(const u4_t *)(q + other + e), kw, qk);
+      else qk = mfma_bf16(ko, *(const u4_t *)(q + own + e), qk);
+    }
+    settle(kk);
+    settle(qk);
+    const int mine = 16 * wv + d;
+    f4_t am, p;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int r = 16 * o + 4 * g4 + x, i = BWD ? r : mine, j = BWD ? mine : r;
+      const float e = exp2_((hi[i] - hi[j]) + (lo[i] - lo[j]));
+      am[x] = j < i ? be[i] * e * kk[x] : 0.f;
+      p[x] = j <= i ? e * qk[x] : 0.f;
+    }
+    if (BWD) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) As[16 * o + 4 * g4 + x][mine] = am[x];
+      const Pair4 s = split4(p);
+      *(u2_t *)&Ps[0][mine][16 * o + 4 * g4] = s.hi;
+      *(u2_t *)&Ps[BWD ? 1 : 0][mine][16 * o + 4 * g4] = s.lo;
+    } else {
+      *(f4_t *)&As[mine][16 * o + 4 * g4] = am;
+      *(u2_t *)&Ps[0][mine][16 * o + 4 * g4] = pack4_h(p);
+    }
+  }
+  __syncthreads();
+  if (lane < 16) {
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float s = d == i ? 1.f : 0.f;
+#pragma unroll
+      for (int j = 0; j < i; ++j) s = fmaf(-As[16 * wv + i][16 * wv + j], x[j], s);
+      x[i] = s;
+      Ts[16 * wv + i][16 * wv + d] = s;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) *(f4_t *)&Tt[16 * wv + d][16 * wv + i] = f4_t{x[i], x[i + 1], x[i + 2], x[i + 3]};
+  }
+  __syncthreads();
+  const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+  if (wv < 2) {  // neighbours: block (2 wv + 1, 2 wv)
+    const int r = 32 * wv + 16, c = 32 * wv;
+    f4_t x = mma_f32(&As[r + d][c + 4 * g4], &Tt[c + d][c + 4 * g4], zero);
+    settle(x);
+    *(f4_t *)&Xt[16 * wv + d][4 * g4] = x;
+  }
+  __syncthreads();
+  if (wv < 2) {
+    const int r = 32 * wv + 16, c = 32 * wv;
+    f4_t x = mma_f32(&Ts[r + d][r + 4 * g4], &Xt[16 * wv + d][4 * g4], zero);
+    settle(x);
+    x = -x;
+    *(f4_t *)&Tt[c + d][r + 4 * g4] = x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Ts[r + 4 * g4 + i][c + d] = x[i];
+  }
+  __syncthreads();
+  const int r = wv >> 1, c = wv & 1;  // tile (2 + r, c)
+  {
+    f4_t x = zero;
+    if (c == 0) x = mma_f32(&As[32 + 16 * r + d][4 * g4], &Tt[d][4 * g4], x);
+    x = mma_f32(&As[32 + 16 * r + d][16 + 4 * g4], &Tt[16 * c + d][16 + 4 * g4], x);
+    settle(x);
+    *(f4_t *)&Xt[16 * c + d][16 * r + 4 * g4] = x;
+  }
+  __syncthreads();
+  {
+    f4_t x = mma_f32(&Ts[32 + 16 * r + d][32 + 4 * g4], &Xt[16 * c + d][4 * g4], zero);
+    if (r == 1) x = mma_f32(&Ts[48 + d][48 + 4 * g4], &Xt[16 * c + d][16 + 4 * g4], x);
+    settle(x);
+    x = -x;
+    *(f4_t *)&Tt[16 * c + d][32 + 16 * r + 4 * g4] = x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Ts[32 + 16 * r + 4 * g4 + i][16 * c + d] = x[i];
+  }
+  __syncthreads();
+  half_t *Tm = mats + (size_t)blockIdx.x * 2 * kMat, *Pm = Tm + kMat;
+  const int me = 16 * wv + d;
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    if (BWD ? (kb == 0 && wv >= 2) : (kb == 1 && wv < 2)) continue;  // (zero)
+    const int c0 = 32 * kb + 8 * g4;
+    u4_t th, tl, ph, pl;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f4_t x = *(const f4_t *)(BWD ? &Tt[me][c0 + 4 * u] : &Ts[me][c0 + 4 * u]);
+      u2_t y = *(const u2_t *)&Ps[0][me][c0 + 4 * u], z = *(const u2_t *)&Ps[BWD ? 1 : 0][me][c0 + 4 * u];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int o = c0 + 4 * u + v;
+        if (BWD ? o < me : o > me) x[v] = 0.f;  // (tiles beyond the diagonal have not been written)
+      }
+      if (BWD ? c0 + 4 * u + 3 < me - d : c0 + 4 * u > me - d + 15) y = z = u2_t{0u, 0u};
+      const Pair4 s = split4(x);
+      th[2 * u] = s.hi.x; th[2 * u + 1] = s.hi.y;
+      tl[2 * u] = s.lo.x; tl[2 * u + 1] = s.lo.y;
+      ph[2 * u] = y.x; ph[2 * u + 1] = y.y;
+      pl[2 * u] = z.x; pl[2 * u + 1] = z.y;
+    }
+    *(u4_t *)(Tm + mat_at(wv, kb, 0) + lane * 8) = th;
+    *(u4_t *)(Tm + mat_at(wv, kb, 1) + lane * 8) = tl;
+    *(u4_t *)(Pm + mat_at(wv, kb, 0) + lane * 8) = ph;
+    if (BWD) *(u4_t *)(Pm + mat_at(wv, kb, 1) + lane * 8) = pl;
+  }
+}
+
+// ------------------------------------------------------------------ forward, chunks in order
+// Wave w has the chunk's steps 16 w .. 16 w + 15 in products over steps, and tiles w, w + 4, .. of the state.
+template <int K, int VB>
+struct Scan {
+  static constexpr int KB = K / 32, KT = K / 16, VT = VB / 16, NT = KT * VT, PW = (NT + 3) / 4;
+  static constexpr int LK = K + 8;
+};
+// Where the operand that holds 16 rows x 32 columns of V goes: [V / 32][tiles][lane][8]; with VB = 16 a
+// workgroup has one half of the lanes.
+template <int VB>
+__device__ __forceinline__ bool frag_at(int part, int tiles, int tile, size_t &o) {
+  const int lane = threadIdx.x & 63;
+  if constexpr (VB == 32) {
+    o = ((size_t)(part * tiles + tile) * 64 + lane) * 8;
+    return true;
+  } else {
+    o = ((size_t)((part >> 1) * tiles + tile) * 64 + (lane & 31) + 32 * (part & 1)) * 8;
+    return lane < 32;
+  }
+}
+// that operand, from an LDS array [VB][ld] whose columns c0 .. c0 + 15 are its rows
+template <int VB>
+__device__ __forceinline__ h8_t frag_of(const half_t *base, int ld, int c0) {
+  const int lane = threadIdx.x & 63, d = lane & 15, g = VB == 32 ? lane >> 4 : (lane >> 4) & 1;
+  const half_t *p = base + (8 * g + (d >> 2)) * ld + c0 + 4 * (d & 3);
+  return tr8(p, p + 4 * ld);
+}
+
+template <int K, int VB>
+constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC) * 2; }
+
+template <int K, int VB>
+__global__ void __launch_bounds__(256, 2)
+    delta_half_fwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const half_t *__restrict__ mats,
+                          half_t *__restrict__ states, half_t *__restrict__ rows_u) {
+  using S = Scan<K, VB>;
+  constexpr int KB = S::KB, KT = S::KT, VT = S::VT, NT = S::NT, PW = S::PW, LK = S::LK;
+  extern __shared__ __align__(16) char lds[];
+  half_t *ks = (half_t *)lds, *Ht = ks + C * LK, *Hl = Ht + VB * LK, *Rt = Hl + VB * LK, *Rl = Rt + VB * LC;
+  half_t *Ut = Rl + VB * LC, *Wt = Ut + VB * LC, *Wl = Wt + VB * LC;
+  int unit, part;
+  if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
+  const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int d = lane & 15, g4 = lane >> 4;
+  const bool two = wv >= 2;  // (T and P are lower triangular: the first two waves have no steps above 31)
+  const size_t qrow = (size_t)a.Nqk * K, qbase = (size_t)b * a.T * qrow + (size_t)nq * K + 8 * g4;
+  const size_t vrow = (size_t)a.N * a.V, vbase = (size_t)b * a.T * vrow + (size_t)n * a.V + part * VB;
+  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k, *v = (const unsigned short *)a.v;
+  const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+
+  f4_t H[PW];
+#pragma unroll
+  for (int p = 0; p < PW; ++p) {
+    const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+    H[p] = zero;
+    if (a.H0 && t < NT)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        H[p][x] = a.H0[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d];
+  }
+  u4_t nk[KB], nqr[KB], nT[4], nP[2];
+  unsigned short nv[VT][4];
+  f4_t nge, ngl, nbe;
+  float ng1, ngc;
+  auto fetch = [&](int ch) {
+    const int t0 = ch * C;
+    const size_t at = (size_t)unit * chunks + ch, r = qbase + (size_t)min(t0 + 16 * wv + d, a.T - 1) * qrow;
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      nk[i] = *(const u4_t *)(k + r + 32 * i);
+      nqr[i] = *(const u4_t *)(q + r + 32 * i);
+    }
+    const half_t *Tm = mats + at * 2 * kMat + lane * 8, *Pm = Tm + kMat;
+    nT[0] = *(const u4_t *)(Tm + mat_at(wv, 0, 0));
+    nT[1] = *(const u4_t *)(Tm + mat_at(wv, 0, 1));
+    nP[0] = *(const u4_t *)(Pm + mat_at(wv, 0, 0));
+    const int kb = two ? 1 : 0;  // (unconditional: the first two waves read their only block again)
+    nT[2] = *(const u4_t *)(Tm + mat_at(wv, kb, 0));
+    nT[3] = *(const u4_t *)(Tm + mat_at(wv, kb, 1));
+    nP[1] = *(const u4_t *)(Pm + mat_at(wv, kb, 0));
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const size_t rv = vbase + (size_t)min(t0 + 16 * wv + 4 * g4 + x, a.T - 1) * vrow + d;
+#pragma unroll
+      for (int t = 0; t < VT; ++t) nv[t][x] = v[rv + 16 * t];
+    }
+    const float *gt = gates + at * kGates + 16 * wv;
+    nge = *(const f4_t *)(gt + 4 * g4);
+    ngl = *(const f4_t *)(gt + C + 4 * g4);
+    nbe = *(const f4_t *)(gt + 4 * C + 4 * g4);
+    ng1 = gt[d];
+    ngc = gates[at * kGates + C - 1];
+  };
+  auto put_state = [&]() {
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+      if (t < NT) {
+        const Pair4 s = split4(H[p]);
+        *(u2_t *)&Ht[(16 * vt + d) * LK + 16 * kt + 4 * g4] = s.hi;
+        *(u2_t *)&Hl[(16 * vt + d) * LK + 16 * kt + 4 * g4] = s.lo;
+      }
+    }
+  };
+  put_state();
+  if (chunks > 0) fetch(0);
+  for (int ch = 0; ch < chunks; ++ch) {
+    const int t0 = ch * C;
+    const size_t at = (size_t)unit * chunks + ch;
+    h8_t kf[KB], qf[KB], Tf[4], Pf[2];
+    f4_t vf[VT];
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      kf[i] = bf16_to_h8(nk[i]);
+      qf[i] = bf16_to_h8(nqr[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Tf[i] = __builtin_bit_cast(h8_t, nT[i]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) Pf[i] = __builtin_bit_cast(h8_t, nP[i]);
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) vf[t][x] = bf16_bits_to_f32(nv[t][x]);
+    const f4_t ge = nge, gl = ngl, be = nbe;
+    const float g1 = ng1, gc = ngc;
+    lds_barrier();  // the state is there, and k of the chunk before has been read
+    fetch(min(ch + 1, chunks - 1));
+#pragma unroll
+    for (int i = 0; i < KB; ++i) *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
+    // R = beta (v - e^G K H): D[step][column]
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      f4_t x = zero;
+#pragma unroll
+      for (int i = 0; i < KB; ++i) {
+        const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
+        x = mfma_k32(kf[i], ld8(Ht + o), x);
+        x = mfma_k32(kf[i], ld8(Hl + o), x);
+      }
+      settle(x);
+      const Pair4 s = split4(be * (vf[t] - ge * x));
+      *(u2_t *)&Rt[(16 * t + d) * LC + 16 * wv + 4 * g4] = s.hi;
+      *(u2_t *)&Rl[(16 * t + d) * LC + 16 * wv + 4 * g4] = s.lo;
+    }
+    if (states) {
+      for (int kt = wv; kt < KT; kt += 4) {
+        size_t o;
+        const h8_t f = frag_of<VB>(Ht, LK, 16 * kt);
+        if (frag_at<VB>(part, KT, kt, o)) *(h8_t *)(states + at * K * a.V + o) = f;
+      }
+    }
+    lds_barrier();
+    // (Q H)^T: D[column][step], off the chain
+    f4_t y[VT];
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      y[t] = zero;
+      if (a.write_y)
+#pragma unroll
+        for (int i = 0; i < KB; ++i) y[t] = mfma_k32(ld8(Ht + (16 * t + d) * LK + 32 * i + 8 * g4), qf[i], y[t]);
+      settle(y[t]);
+    }
+    // U = T R: D[step][column]
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      const int o = (16 * t + d) * LC + 8 * g4;
+      f4_t u = zero;
+      {
+        const h8_t rh = ld8(Rt + o), rl = ld8(Rl + o);
+        u = mfma_k32(Tf[0], rh, u);
+        u = mfma_k32(Tf[1], rh, u);
+        u = mfma_k32(Tf[0], rl, u);
+      }
+      if (two) {
+        const h8_t rh = ld8(Rt + o + 32), rl = ld8(Rl + o + 32);
+        u = mfma_k32(Tf[2], rh, u);
+        u = mfma_k32(Tf[3], rh, u);
+        u = mfma_k32(Tf[2], rl, u);
+      }
+      settle(u);
+      const int w = (16 * t + d) * LC + 16 * wv + 4 * g4;
+      *(u2_t *)&Ut[w] = pack4_h(u);
+      const Pair4 s = split4(gl * u);
+      *(u2_t *)&Wt[w] = s.hi;
+      *(u2_t *)&Wl[w] = s.lo;
+    }
+    lds_barrier();
+    // H = e^{G_C} H + K^T W: D[row][column]
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+      if (t < NT) {
+        f4_t x = gc * H[p];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const h8_t kT = ld8_tr(ks, LK, 32 * kb, 16 * kt);
+          const int o = (16 * vt + d) * LC + 32 * kb + 8 * g4;
+          x = mfma_k32(kT, ld8(Wt + o), x);
+          x = mfma_k32(kT, ld8(Wl + o), x);
+        }
+        settle(x);
+        H[p] = x;
+      }
+    }
+    put_state();
+    // y = e^G (Q H)^T + (P U)^T, and U for the backward
+    if (a.write_y) {
+      const int step = t0 + 16 * wv + d;
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        const int o = (16 * t + d) * LC + 8 * g4;
+        f4_t x = mfma_k32(ld8(Ut + o), Pf[0], g1 * y[t]);
+        if (two) x = mfma_k32(ld8(Ut + o + 32), Pf[1], x);
+        settle(x);
+        if (step < a.T)
+          *(u2_t *)((unsigned short *)a.y + vbase + (size_t)step * vrow + 16 * t + 4 * g4) =
+              u2_t{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])};
+      }
+    }
+    if (rows_u) {
+      size_t o;
+      const h8_t f = frag_of<VB>(Ut, LC, 16 * wv);
+      if (frag_at<VB>(part, 4, wv, o)) *(h8_t *)(rows_u + at * C * a.V + o) = f;
+    }
+  }
+  if (a.HT)
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+      if (t < NT)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          a.HT[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d] = H[p][x];
+    }
+}
+
+// ------------------------------------------------------------------ backward, chunks in reverse order
+// Gradients of a chunk are brought near one by s, a power of two from the largest |dH| and |dy| of the
+// workgroup's columns: with unit keys nothing below exceeds some hundreds then, and the pairs' 2^-25 is small.
+template <int K, int VB>
+constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC) * 2 + 16; }
+
+template <int K, int VB>
+__global__ void __launch_bounds__(256, 2)
+    delta_half_bwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const half_t *__restrict__ mats,
+                          half_t *__restrict__ dstates, half_t *__restrict__ rows_z, float *__restrict__ scales) {
+  using S = Scan<K, VB>;
+  constexpr int KB = S::KB, KT = S::KT, VT = S::VT, NT = S::NT, PW = S::PW, LK = S::LK;
+  extern __shared__ __align__(16) char lds[];
+  half_t *ks = (half_t *)lds, *qs = ks + C * LK, *Ht = qs + C * LK, *Hl = Ht + VB * LK, *Yt = Hl + VB * LK;
+  half_t *Wt = Yt + VB * LC, *Wl = Wt + VB * LC, *Ut = Wl + VB * LC, *Ul = Ut + VB * LC;
+  half_t *Zt = Wt, *Zl = Wl;  // (W has been read when Z comes)
+  float *red = (float *)(Ul + VB * LC);
+  int unit, part;
+  if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
+  const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int d = lane & 15, g4 = lane >> 4;
+  const bool two = wv < 2;  // (transposed: the last two waves have no steps below 32)
+  const size_t qrow = (size_t)a.Nqk * K, qbase = (size_t)b * a.T * qrow + (size_t)nq * K + 8 * g4;
+  const size_t vrow = (size_t)a.N * a.V, vbase = (size_t)b * a.T * vrow + (size_t)n * a.V + part * VB;
+  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k;
+  const unsigned short *dy = (const unsigned short *)a.dy;
+  const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+
+  f4_t D[PW];
+#pragma unroll
+  for (int p = 0; p < PW; ++p) {
+    const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+    D[p] = zero;
+    if (a.dHT && t < NT)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        D[p][x] = a.dHT[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d];
+  }
+  u4_t nk[KB], nqr[KB], nT[4], nP[4];
+  unsigned short ny[VT][4];
+  f4_t nge, ngl, nbe;
+  float nb1, ngc, nom;
+  auto fetch = [&](int ch) {
+    const int t0 = ch * C;
+    const size_t at = (size_t)unit * chunks + ch, r = qbase + (size_t)min(t0 + 16 * wv + d, a.T - 1) * qrow;
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      nk[i] = *(const u4_t *)(k + r + 32 * i);
+      nqr[i] = *(const u4_t *)(q + r + 32 * i);
+    }
+    const half_t *Tm = mats + at * 2 * kMat + lane * 8, *Pm = Tm + kMat;
+    const int kb = two ? 0 : 1;  // (unconditional: the last two waves read their only block again)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      nT[i] = *(const u4_t *)(Tm + mat_at(wv, 1, i));
+      nP[i] = *(const u4_t *)(Pm + mat_at(wv, 1, i));
+      nT[2 + i] = *(const u4_t *)(Tm + mat_at(wv, kb, i));
+      nP[2 + i] = *(const u4_t *)(Pm + mat_at(wv, kb, i));
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const size_t rv = vbase + (size_t)min(t0 + 16 * wv + 4 * g4 + x, a.T - 1) * vrow + d;
+#pragma unroll
+      for (int t = 0; t < VT; ++t) ny[t][x] = dy[rv + 16 * t];
+    }
+    const float *gt = gates + at * kGates + 16 * wv;
+    nge = *(const f4_t *)(gt + 4 * g4);
+    ngl = *(const f4_t *)(gt + C + 4 * g4);
+    nbe = *(const f4_t *)(gt + 4 * C + 4 * g4);
+    nb1 = gt[4 * C + d];
+    nom = gate_unit(gates[at * kGates + 2 * C]);
+    ngc = nom * gates[at * kGates + C - 1];
+  };
+  if (chunks > 0) fetch(chunks - 1);
+  for (int ch = chunks - 1; ch >= 0; --ch) {
+    const int t0 = ch * C;
+    const size_t at = (size_t)unit * chunks + ch;
+    h8_t kf[KB], Tf[4], Pf[4];
+    f4_t yf[VT];
+    float top = 0.f;
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        yf[t][x] = t0 + 16 * wv + 4 * g4 + x < a.T ? bf16_bits_to_f32(ny[t][x]) : 0.f;
+        top = fmaxf(top, fabsf(yf[t][x]));
+      }
+#pragma unroll
+    for (int p = 0; p < PW; ++p)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) top = fmaxf(top, fabsf(D[p][x]));
+    top = group_max_nonneg<64>(top);
+    if (lane == 0) red[wv] = top;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      Tf[i] = __builtin_bit_cast(h8_t, nT[i]);
+      Pf[i] = __builtin_bit_cast(h8_t, nP[i]);
+    }
+    const f4_t ge = nge, gl = ngl, be = nbe;
+    const float b1 = nb1, gc = ngc, om = nom;
+    lds_barrier();  // (and everything of the chunk before has been read)
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const int e = min(max(ilog2f(top), -100), 100);
+    const float s = pow2i(-e), inv = pow2i(e);
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      kf[i] = bf16_to_h8(nk[i]);
+      *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
+      *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = bf16_to_h8(nqr[i]);
+    }
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+      if (t < NT) {
+        const Pair4 x = split4(s * D[p]);
+        *(u2_t *)&Ht[(16 * vt + d) * LK + 16 * kt + 4 * g4] = x.hi;
+        *(u2_t *)&Hl[(16 * vt + d) * LK + 16 * kt + 4 * g4] = x.lo;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      const int o = (16 * t + d) * LC + 16 * wv + 4 * g4;
+      const f4_t y = s * yf[t];
+      const Pair4 x = split4(ge * y);
+      *(u2_t *)&Yt[o] = pack4_h(y);
+      *(u2_t *)&Wt[o] = x.hi;
+      *(u2_t *)&Wl[o] = x.lo;
+    }
+    lds_barrier();
+    fetch(max(ch - 1, 0));
+    // dU = P^T dY + e^{G_C - G} K dH: D[step][column]
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      f4_t u = zero;
+#pragma unroll
+      for (int i = 0; i < KB; ++i) {
+        const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
+        u = mfma_k32(kf[i], ld8(Ht + o), u);
+        u = mfma_k32(kf[i], ld8(Hl + o), u);
+      }
+      settle(u);
+      u = gl * u;
+      const int o = (16 * t + d) * LC + 8 * g4;
+      {
+        const h8_t y = ld8(Yt + o + 32);
+        u = mfma_k32(Pf[0], y, u);
+        u = mfma_k32(Pf[1], y, u);
+      }
+      if (two) {
+        const h8_t y = ld8(Yt + o);
+        u = mfma_k32(Pf[2], y, u);
+        u = mfma_k32(Pf[3], y, u);
+      }
+      settle(u);
+      const Pair4 x = split4(u);
+      const int w = (16 * t + d) * LC + 16 * wv + 4 * g4;
+      *(u2_t *)&Ut[w] = x.hi;
+      *(u2_t *)&Ul[w] = x.lo;
+    }
+    // Q^T e^G dY, off the chain
+    f4_t acc[PW];
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+      acc[p] = zero;
+      if (t < NT) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const h8_t qT = ld8_tr(qs, LK, 32 * kb, 16 * kt);
+          const int o = (16 * vt + d) * LC + 32 * kb + 8 * g4;
+          acc[p] = mfma_k32(qT, ld8(Wt + o), acc[p]);
+          acc[p] = mfma_k32(qT, ld8(Wl + o), acc[p]);
+        }
+        settle(acc[p]);
+      }
+    }
+    for (int kt = wv; kt < KT; kt += 4) {
+      size_t o;
+      const h8_t f = frag_of<VB>(Ht, LK, 16 * kt);
+      if (frag_at<VB>(part, KT, kt, o)) *(h8_t *)(dstates + at * K * a.V + o) = f;
+    }
+    if (threadIdx.x == 0) scales[at * (a.V / VB) + part] = s;
+    lds_barrier();
+    // Z = T^T dU, as D[step][column] for the state and as D[column][step] for what is written
+    f4_t z[VT];
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      const int o = (16 * t + d) * LC + 8 * g4;
+      f4_t x = zero;
+      z[t] = zero;
+      {
+        const h8_t uh = ld8(Ut + o + 32), ul = ld8(Ul + o + 32);
+        x = mfma_k32(Tf[0], uh, x);
+        x = mfma_k32(Tf[1], uh, x);
+        x = mfma_k32(Tf[0], ul, x);
+        z[t] = mfma_k32(uh, Tf[0], z[t]);
+        z[t] = mfma_k32(uh, Tf[1], z[t]);
+        z[t] = mfma_k32(ul, Tf[0], z[t]);
+      }
+      if (two) {
+        const h8_t uh = ld8(Ut + o), ul = ld8(Ul + o);
+        x = mfma_k32(Tf[2], uh, x);
+        x = mfma_k32(Tf[3], uh, x);
+        x = mfma_k32(Tf[2], ul, x);
+        z[t] = mfma_k32(uh, Tf[2], z[t]);
+        z[t] = mfma_k32(uh, Tf[3], z[t]);
+        z[t] = mfma_k32(ul, Tf[2], z[t]);
+      }
+      settle(x);
+      settle(z[t]);
+      const Pair4 w = split4(-(be * ge) * x);
+      const int o2 = (16 * t + d) * LC + 16 * wv + 4 * g4;
+      *(u2_t *)&Zt[o2] = w.hi;
+      *(u2_t *)&Zl[o2] = w.lo;
+    }
+    lds_barrier();
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+      if (t < NT) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const h8_t kT = ld8_tr(ks, LK, 32 * kb, 16 * kt);
+          const int o = (16 * vt + d) * LC + 32 * kb + 8 * g4;
+          acc[p] = mfma_k32(kT, ld8(Zt + o), acc[p]);
+          acc[p] = mfma_k32(kT, ld8(Zl + o), acc[p]);
+        }
+        settle(acc[p]);
+        D[p] = gc * D[p] + (inv * om) * acc[p];
+      }
+    }
+    const int step = t0 + 16 * wv + d;
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      // (a lane's four columns are half of the eight that the operand's lane d + 16 (column / 8) holds)
+      const int c = (VB == 32 ? 0 : 16 * (part & 1)) + 16 * t + 4 * g4, v32 = VB == 32 ? part : part >> 1;
+      *(u2_t *)(rows_z + at * C * a.V + ((size_t)(v32 * 4 + wv) * 64 + d + 16 * (c >> 3)) * 8 + (c & 7)) = pack4_h(z[t]);
+      if (step < a.T) {
+        const f4_t o = (b1 * inv) * z[t];
+        *(u2_t *)((unsigned short *)a.dv + vbase + (size_t)step * vrow + 16 * t + 4 * g4) =
+            u2_t{pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3])};
+      }
+    }
+  }
+  if (a.dH0)
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
+      if (t < NT)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          a.dH0[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d] = D[p][x];
+    }
+}
+
+// ------------------------------------------------------------------ dq, dk, dg, dbeta of one chunk
+// Wave w has the chunk's steps 16 w .. 16 w + 15 and all of K: D[row of K][step].
+template <int K>
+constexpr int lds_grad() { return (2 * C * (K + 8) + 3 * C * LC) * 2 + (6 * C + 4 * 4) * 4; }
+
+__device__ __forceinline__ float dot8(h8_t a, h8_t b, float c) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2)
+    c = __builtin_amdgcn_fdot2(h2_t{a[i], a[i + 1]}, h2_t{b[i], b[i + 1]}, c, false);
+  return c;
+}
+
+template <int K>
+__global__ void __launch_bounds__(256, 2)
+    delta_half_grad_kernel(DeltaArgs a, int chunks, int vbs, const float *__restrict__ gates,
+                           const half_t *__restrict__ states, const half_t *__restrict__ rows_u,
+                           const half_t *__restrict__ dstates, const half_t *__restrict__ rows_z,
+                           const float *__restrict__ scales, float *__restrict__ dq_heads, float *__restrict__ dk_heads) {
+  constexpr int KB = K / 32, KT = K / 16, LK = K + 8;
+  extern __shared__ __align__(16) char lds[];
+  half_t *ks = (half_t *)lds, *qs = ks + C * LK, *S1 = qs + C * LK, *S2 = S1 + C * LC, *Sb = S2 + C * LC;
+  float *ge = (float *)(Sb + C * LC), *red = ge + 5 * C;  // e^G, e^{G_C - G}, hi, lo, beta;  [4][4] and dG [C]
+  const int unit = blockIdx.x / chunks, ch = blockIdx.x - unit * chunks, t0 = ch * C;
+  const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int d = lane & 15, g4 = lane >> 4;
+  const size_t at = (size_t)blockIdx.x;
+  const size_t qrow = (size_t)a.Nqk * K, qbase = (size_t)b * a.T * qrow + (size_t)nq * K;
+  const size_t vrow = (size_t)a.N * a.V, vbase = (size_t)b * a.T * vrow + (size_t)n * a.V + 8 * g4;
+  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k;
+  const unsigned short *dy = (const unsigned short *)a.dy, *v = (const unsigned short *)a.v;
+  const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+  const int own = t0 + 16 * wv + d, clamped = min(own, a.T - 1);
+#pragma unroll
+  for (int i = 0; i < KB; ++i) {
+    const size_t o = qbase + (size_t)clamped * qrow + 32 * i + 8 * g4;
+    *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = bf16_to_h8(*(const u4_t *)(k + o));
+    *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = bf16_to_h8(*(const u4_t *)(q + o));
+  }
+  for (int i = threadIdx.x; i < kGates; i += 256) ge[i] = gates[at * kGates + i];
+  // the chunk's common power of two: that of the block with the largest gradients
+  const int blocks = a.V / vbs;
+  float sc = scales[at * blocks];
+  for (int i = 1; i < blocks; ++i) sc = fminf(sc, scales[at * blocks + i]);
+
+  f4_t dq[KT], as[KT], kept[KT], s1[4], s2[4];
+#pragma unroll
+  for (int i = 0; i < KT; ++i) dq[i] = as[i] = kept[i] = zero;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s1[i] = s2[i] = zero;
+  float zv = 0.f, hd = 0.f;
+  for (int vb = 0; vb < a.V / 32; ++vb) {
+    const float f = sc / scales[at * blocks + (vbs == 32 ? vb : 2 * vb + (g4 >> 1))];
+    const half_t fh = (half_t)f;
+    const h8_t f8 = {fh, fh, fh, fh, fh, fh, fh, fh};
+    const half_t *U = rows_u + at * C * a.V + (size_t)vb * 4 * 512 + lane * 8;
+    const h8_t z = ld8(rows_z + at * C * a.V + (size_t)(vb * 4 + wv) * 512 + lane * 8) * f8;
+    const u4_t yr = *(const u4_t *)(dy + vbase + (size_t)clamped * vrow + 32 * vb);
+    const u4_t vr = *(const u4_t *)(v + vbase + (size_t)clamped * vrow + 32 * vb);
+    float yy[8], vv[8];
+    bf16x8_to_f32(yr, yy);
+    bf16x8_to_f32(vr, vv);
+    const float sy = own < a.T ? sc : 0.f;
+    const u4_t yp = {pack2_h(own < a.T ? sy * yy[0] : 0.f, own < a.T ? sy * yy[1] : 0.f),
+                     pack2_h(own < a.T ? sy * yy[2] : 0.f, own < a.T ? sy * yy[3] : 0.f),
+                     pack2_h(own < a.T ? sy * yy[4] : 0.f, own < a.T ? sy * yy[5] : 0.f),
+                     pack2_h(own < a.T ? sy * yy[6] : 0.f, own < a.T ? sy * yy[7] : 0.f)};
+    const h8_t y = __builtin_bit_cast(h8_t, yp);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) zv = fmaf((float)z[i], vv[i], zv);
+    h8_t u = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)  // D[j][i], j <= i
+      if (j <= wv) {
+        const h8_t uj = ld8(U + j * 512);
+        s1[j] = mfma_k32(uj, y, s1[j]);
+        s2[j] = mfma_k32(uj, z, s2[j]);
+        u = uj;  // (the last one is my own)
+      }
+    const half_t *h0 = states + at * K * a.V + (size_t)vb * KT * 512 + lane * 8;
+    const half_t *h1 = dstates + at * K * a.V + (size_t)vb * KT * 512 + lane * 8;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const h8_t x0 = ld8(h0 + i * 512), x1 = ld8(h1 + i * 512) * f8;
+      dq[i] = mfma_k32(x0, y, dq[i]);
+      as[i] = mfma_k32(x0, z, as[i]);
+      kept[i] = mfma_k32(x1, u, kept[i]);
+      if ((i & 3) == wv) hd = dot8(x0, x1, hd);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    settle(s1[i]);
+    settle(s2[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < KT; ++i) {
+    settle(dq[i]);
+    settle(as[i]);
+    settle(kept[i]);
+  }
+  __syncthreads();
+  // S1, S2 masked; their largest entry, so that they can be fp16 whatever U is
+  const int i = 16 * wv + d;
+  float top = 0.f;
+#pragma unroll
+  for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int j = 16 * jt + 4 * g4 + x;
+      const float e = exp2_((ge[2 * C + i] - ge[2 * C + j]) + (ge[3 * C + i] - ge[3 * C + j]));
+      s1[jt][x] = j <= i ? e * s1[jt][x] : 0.f;
+      s2[jt][x] = j < i ? -e * s2[jt][x] : 0.f;
+      top = fmaxf(top, fmaxf(fabsf(s1[jt][x]), fabsf(s2[jt][x])));
+    }
+  top = group_max_nonneg<64>(top);
+  zv += __shfl_xor(zv, 16, 64);
+  zv += __shfl_xor(zv, 32, 64);
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) hd += __shfl_xor(hd, m, 64);
+  if (lane == 0) {
+    red[wv * 4] = top;
+    red[wv * 4 + 1] = hd;
+  }
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[4]), fmaxf(red[8], red[12]));
+  const int ex = min(max(ilog2f(top), -100), 100);
+  const float ss = pow2i(-ex), sinv = pow2i(ex), bt = ge[4 * C + i], gt = ge[C + i];
+  const float om = gate_unit(ge[2 * C]), gm = om * ge[i];
+#pragma unroll
+  for (int jt = 0; jt < 4; ++jt) {  // (the last tile of an even wave's pair is zero)
+    const int o = i * LC + 16 * jt + 4 * g4;
+    *(u2_t *)&S1[o] = pack4_h(ss * s1[jt]);
+    *(u2_t *)&S2[o] = pack4_h(ss * s2[jt]);
+    *(u2_t *)&Sb[o] = pack4_h((ss * bt) * s2[jt]);
+  }
+  __syncthreads();
+  const bool heads = a.N != a.Nqk;
+  const float inv = 1.f / sc;
+  float dG = 0.f, kb1 = 0.f, tail = 0.f;
+  h8_t row1[2], row2[2], col1[2], colb[2];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    row1[kb] = ld8(S1 + i * LC + 32 * kb + 8 * g4);
+    row2[kb] = ld8(S2 + i * LC + 32 * kb + 8 * g4);
+    col1[kb] = ld8_tr(S1, LC, 32 * kb, 16 * wv);
+    colb[kb] = ld8_tr(Sb, LC, 32 * kb, 16 * wv);
+  }
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const f4_t kd = kept[kt];
+    f4_t x = (ss * gm) * dq[kt], y = (-ss * gm) * as[kt], w = (ss * gt) * kd;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const h8_t kT = ld8_tr(ks, LK, 32 * kb, 16 * kt), qT = ld8_tr(qs, LK, 32 * kb, 16 * kt);
+      x = mfma_k32(kT, row1[kb], x);
+      y = mfma_k32(kT, row2[kb], y);
+      w = mfma_k32(qT, col1[kb], w);
+      w = mfma_k32(kT, colb[kb], w);
+    }
+    settle(x);
+    settle(y);
+    settle(w);
+    const h4_t qv = *(const h4_t *)&qs[i * LK + 16 * kt + 4 * g4], kv = *(const h4_t *)&ks[i * LK + 16 * kt + 4 * g4];
+    f4_t o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float qx = (float)qv[r], kx = (float)kv[r];
+      x[r] *= sinv;
+      y[r] *= sinv;
+      w[r] *= sinv;
+      o[r] = fmaf(bt, y[r], w[r]);
+      dG = fmaf(qx, x[r], dG);
+      dG = fmaf(kx, fmaf(bt, y[r], -w[r]), dG);
+      kb1 = fmaf(kx, y[r], kb1);
+      tail = fmaf(gt * kx, kd[r], tail);
+    }
+    if (own < a.T) {
+      const size_t m = ((size_t)b * a.T + own) * (heads ? a.N : a.Nqk) * K + (size_t)(heads ? n : nq) * K + 16 * kt + 4 * g4;
+      x *= inv;
+      o *= inv;
+      if (heads) {
+        *(f4_t *)&dq_heads[m] = x;
+        *(f4_t *)&dk_heads[m] = o;
+      } else {
+        *(u2_t *)((unsigned short *)a.dq + m) = u2_t{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])};
+        *(u2_t *)((unsigned short *)a.dk + m) = u2_t{pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3])};
+      }
+    }
+  }
+  dG += __shfl_xor(dG, 16, 64);
+  dG += __shfl_xor(dG, 32, 64);
+  kb1 += __shfl_xor(kb1, 16, 64);
+  kb1 += __shfl_xor(kb1, 32, 64);
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) tail += __shfl_xor(tail, m, 64);
+  if (lane == 0) red[wv * 4 + 2] = tail;
+  if (g4 == 0) red[16 + i] = dG;
+  if (g4 == 0 && own < a.T)
+    ((__hip_bfloat16 *)a.dbeta)[((size_t)b * a.T + own) * a.N + n] = __float2bfloat16(inv * (zv + kb1));
+  __syncthreads();
+  if (wv == 0) {  // sums over the steps behind, in 64 bits; <H_C, dH> at the last one
+    double s = (double)red[16 + lane];
+    if (lane == C - 1)
+      for (int w = 0; w < 4; ++w) s += (double)(om * ge[C - 1]) * red[4 * w + 1] + red[4 * w + 2];
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+      const double o = __shfl_down(s, m, 64);
+      if (lane + m < 64) s += o;
+    }
+    if (t0 + lane < a.T)
+      ((__hip_bfloat16 *)a.dg)[((size_t)b * a.T + t0 + lane) * a.N + n] = __float2bfloat16((float)(inv * s));
+  }
+}
+
+// ------------------------------------------------------------------ launches
+struct Ws {
+  float *gates;
+  half_t *mats, *dstates, *rows_z;
+  float *scales, *dqh, *dkh;
+};
+Ws carve(const DeltaLayout &l, char *p) {
+  Ws w;
+  w.gates = (float *)p;
+  w.mats = (half_t *)(p += l.gates);
+  w.dstates = (half_t *)(p += l.mats);
+  w.rows_z = (half_t *)(p += l.states);
+  w.scales = (float *)(p += l.rows);
+  w.dqh = (float *)(p += l.scales);
+  w.dkh = (float *)(p += l.heads);
+  return w;
+}
+
+// Columns of V per workgroup of the kernels that run in order
+int columns(const DeltaArgs &a) { (void)a; return 32; }
+
+template <bool BWD>
+hipError_t prep(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
+  hipLaunchKernelGGL(delta_half_prep_kernel<BWD>, dim3((unsigned)(a.B * a.N) * (unsigned)l.chunks), dim3(256), 0, s, a,
+                     l.chunks, w.gates, w.mats);
+  return hipGetLastError();
+}
+template <int K, int VB>
+hipError_t fwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
+  constexpr int lds = lds_fwd<K, VB>();
+  const hipError_t e = set_max_lds_once(delta_half_fwd_kernel<K, VB>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((delta_half_fwd_kernel<K, VB>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a, l.chunks, w.gates, w.mats, (half_t *)a.ckpt,
+                     a.ckpt ? (half_t *)(a.ckpt + l.states) : nullptr);
+  return hipGetLastError();
+}
+template <int K, int VB>
+hipError_t bwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
+  constexpr int lds = lds_bwd<K, VB>(), ldsg = lds_grad<K>();
+  hipError_t e = set_max_lds_once(delta_half_bwd_kernel<K, VB>, lds);
+  if (e == hipSuccess) e = set_max_lds_once(delta_half_grad_kernel<K>, ldsg);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((delta_half_bwd_kernel<K, VB>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a, l.chunks, w.gates, w.mats, w.dstates, w.rows_z, w.scales);
+  if ((e = hipGetLastError()) != hipSuccess || l.chunks == 0) return e;
+  hipLaunchKernelGGL(delta_half_grad_kernel<K>, dim3((unsigned)(a.B * a.N) * (unsigned)l.chunks), dim3(256), ldsg, s, a, l.chunks, VB, w.gates, (const half_t *)a.ckpt,
+                     (const half_t *)(a.ckpt + l.states), w.dstates, w.rows_z, w.scales, w.dqh, w.dkh);
+  return hipGetLastError();
+}
+template <int K>
+hipError_t fwd_k(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
+  return columns(a) == 32 ? fwd_kv<K, 32>(a, l, w, s) : fwd_kv<K, 16>(a, l, w, s);
+}
+template <int K>
+hipError_t bwd_k(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
+  return columns(a) == 32 ? bwd_kv<K, 32>(a, l, w, s) : bwd_kv<K, 16>(a, l, w, s);
+}
+hipError_t scan(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
+  return a.K == 32 ? fwd_k<32>(a, l, w, s) : a.K == 64 ? fwd_k<64>(a, l, w, s) : fwd_k<128>(a, l, w, s);
+}
+
+}  // namespace
+
+// (K = 16 and V = 16 fill half an operand; they run on the fp32 kernels)
+bool delta_half_serves(int K, int V, int io) { return io == 1 && K >= 32 && V >= 32; }
+
+DeltaLayout delta_half_layout(const DeltaArgs &a) {
+  DeltaLayout l;
+  l.C = C;
+  l.chunks = ceil_div(a.T, C);
+  const size_t n = (size_t)a.B * a.N * l.chunks, steps = (size_t)a.B * a.T * a.N;
+  l.gates = align256(n * kGates * sizeof(float));
+  l.mats = align256(n * 2 * kMat * sizeof(half_t));
+  l.states = align256(n * a.K * a.V * sizeof(half_t));
+  l.rows = align256(n * C * a.V * sizeof(half_t));
+  l.scales = align256(n * (a.V / 16) * sizeof(float));
+  l.heads = a.N != a.Nqk ? align256(steps * a.K * sizeof(float)) : 0;
+  return l;
+}
+hipError_t delta_half_fwd(const DeltaArgs &a, hipStream_t s) {
+  const DeltaLayout l = delta_half_layout(a);
+  const Ws w = carve(l, a.ws);
+  const hipError_t e = l.chunks > 0 ? prep<false>(a, l, w, s) : hipSuccess;
+  return e != hipSuccess ? e : scan(a, l, w, s);
+}
+hipError_t delta_half_bwd(const DeltaArgs &a, hipStream_t s) {
+  const DeltaLayout l = delta_half_layout(a);
+  const Ws w = carve(l, a.ws);
+  hipError_t e;
+  if (a.own_ckpt && l.chunks > 0) {
+    DeltaArgs f = a;
+    f.write_y = 0;
+    f.HT = nullptr;
+    if ((e = delta_half_fwd(f, s)) != hipSuccess) return e;
+  }
+  if (l.chunks > 0 && (e = prep<true>(a, l, w, s)) != hipSuccess) return e;
+  e = a.K == 32 ? bwd_k<32>(a, l, w, s) : a.K == 64 ? bwd_k<64>(a, l, w, s) : bwd_k<128>(a, l, w, s);
+  if (e != hipSuccess || l.chunks == 0 || a.N == a.Nqk) return e;
+  BwdArgs h = {};
+  h.B = a.B; h.T = a.T; h.N = a.N; h.Nqk = a.Nqk; h.K = a.K; h.io = a.io;
+  if ((e = generic_head_group_sum(h, w.dqh, a.dq, s)) != hipSuccess) return e;
+  return generic_head_group_sum(h, w.dkh, a.dk, s);
+}
+
+}  // namespace m2rnn
