@@ -11,10 +11,13 @@
 // fp32, are as good as that; what only reaches a bf16 result is one fp16 value of 11 bits.  T is formed in fp32.
 // Gradients may have any magnitude: a chunk's are brought near one by a power of two first.
 //
-// Layout.  Products are D = A B^T with rows contiguous along the contraction: a lane reads eight elements of row
-// (lane % 16) at 8 (lane / 16), and holds rows 4 (lane / 16) .. + 3 of column lane % 16 of D.  What one kernel
-// hands to another (T, P, H, U, dH, Z) is stored as the operands that the reader needs, 16 bytes a lane, 1 KB
-// an operand: no reader goes through LDS for it.
+// Layout.  Products are D = A B^T: a lane gives eight elements of row (lane % 16) of a factor, and holds rows
+// 4 (lane / 16) .. + 3 of column lane % 16 of D.  Which eight of the 32 that are contracted is free, as long as both
+// factors agree: over K and V they are neighbours, 8 (lane / 16) .. + 7; over steps the two groups of four that
+// the lane holds in D of the two 16-step tiles, 4 (lane / 16) .. + 3 and 16 further, so that what is a result is an
+// operand as it stands.  LDS arrays with steps side by side keep them in that order (`place`).
+// What one kernel hands to another (T, P, H, U, dH, Z) is stored as the operands that the reader needs, 16 bytes
+// a lane, 1 KB an operand: no reader goes through LDS for it.
 #include "m2rnn_delta.hpp"
 
 namespace m2rnn {
@@ -63,6 +66,15 @@ __device__ __forceinline__ h8_t tr8(const half_t *p0, const half_t *p1) {
   const h4_t a = lds_ld_tr((const lchar *)p0, 0), b = lds_ld_tr((const lchar *)p1, 0);
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
+// Where the steps 16 tile + 4 (lane / 16) .. + 3 lie in an LDS row
+__device__ __forceinline__ int place(int tile) { return 32 * (tile >> 1) + 8 * ((threadIdx.x & 63) >> 4) + 4 * (tile & 1); }
+// The operand whose 16 rows are columns c0 .. c0 + 15 of an LDS array whose rows are steps, contracted over the
+// steps r0 .. r0 + 31
+__device__ __forceinline__ h8_t ld8_steps(const half_t *base, int ld, int r0, int c0) {
+  const int lane = threadIdx.x & 63, d = lane & 15, g = lane >> 4;
+  const half_t *p = base + (r0 + 4 * g + (d >> 2)) * ld + c0 + 4 * (d & 3);
+  return tr8(p, p + 16 * ld);
+}
 // The operand whose 16 rows are columns c0 .. c0 + 15 of an LDS array, contracted over its rows r0 .. r0 + 31
 __device__ __forceinline__ h8_t ld8_tr(const half_t *base, int ld, int r0, int c0) {
   const int lane = threadIdx.x & 63, d = lane & 15, g = lane >> 4;
@@ -75,27 +87,44 @@ __device__ __forceinline__ h8_t ld8_tr(const half_t *base, int ld, int r0, int c
 constexpr size_t kMat = 4 * 2 * 2 * 64 * 8;  // halfs
 __device__ __forceinline__ size_t mat_at(int tile, int kb, int part) { return (size_t)(((tile * 2 + kb) * 2 + part) * 64) * 8; }
 
-__device__ __forceinline__ f4_t mma_f32(const float *a, const float *b, f4_t c) {
-  const f4_t x = *(const f4_t *)a, y = *(const f4_t *)b;
+__device__ __forceinline__ f4_t mma_f32(f4_t a, f4_t b, f4_t c) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
   return c;
 }
 
 // The inverse of I + A by blocks of 16: the diagonal blocks row by row, then
 //     [ T0 0 ; -T1 A10 T0  T1 ]   for the two pairs of neighbours, and the same with blocks of 32,
-// whose products run on the fp32 matrix instructions.
-template <bool BWD>
-__global__ void __launch_bounds__(256) delta_half_prep_kernel(DeltaArgs a, int chunks, float *__restrict__ gates,
-                                                              half_t *__restrict__ mats) {
-  constexpr int LA = C + 4;
-  __shared__ __align__(16) float As[C][LA], Ts[C][LA], Tt[C][LA], Xt[C / 2][C / 2 + 4];
-  __shared__ __align__(16) half_t Ps[BWD ? 2 : 1][C][LC];
+// whose products run on the fp32 matrix instructions; T takes the place of A in LDS block by block.
+// What bounds it is latency: all loads are issued at once, and 24 KB of LDS leave room for six workgroups per CU.
+template <int K, bool BWD>
+__global__ void __launch_bounds__(256, BWD && K == 128 ? 3 : 4)
+    delta_half_prep_kernel(DeltaArgs a, int chunks, float *__restrict__ gates, half_t *__restrict__ mats) {
+  constexpr int LA = C + 4, KB = K / 32;
+  __shared__ __align__(16) float As[C][LA], Xt[C / 2][C / 2 + 4];
   __shared__ float hi[C], lo[C], be[C];
   const int unit = blockIdx.x / chunks, ch = blockIdx.x - unit * chunks;
   const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
   const int t0 = ch * C, lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int d = lane & 15, g4 = lane >> 4;
+  // forward: wave = tile of i, over j <= i, D[j][i];  backward: wave = tile of j, over i >= j, D[i][j]
+  const size_t row = (size_t)a.Nqk * K, base = (size_t)b * a.T * row + (size_t)nq * K + 8 * g4;
+  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k;
+  auto at = [&](int tile) { return base + (size_t)min(t0 + 16 * tile + d, a.T - 1) * row; };
+  u4_t kw[KB], qw[KB], ko[3][KB], qo[3][KB];
+#pragma unroll
+  for (int e = 0; e < KB; ++e) {
+    kw[e] = *(const u4_t *)(k + at(wv) + 32 * e);
+    qw[e] = *(const u4_t *)(q + at(wv) + 32 * e);
+  }
+#pragma unroll
+  for (int o = 0; o < 3; ++o)
+    if (BWD ? wv + 1 + o < 4 : o < wv)
+#pragma unroll
+      for (int e = 0; e < KB; ++e) {
+        ko[o][e] = *(const u4_t *)(k + at(BWD ? wv + 1 + o : o) + 32 * e);
+        if (BWD) qo[o][e] = *(const u4_t *)(q + at(wv + 1 + o) + 32 * e);
+      }
   if (wv == 0) {
     const bool in = t0 + lane < a.T;
     const size_t e = ((size_t)b * a.T + (in ? t0 + lane : 0)) * a.N + n;
@@ -113,23 +142,19 @@ __global__ void __launch_bounds__(256) delta_half_prep_kernel(DeltaArgs a, int c
     gt[4 * C + lane] = beta;
   }
   __syncthreads();
-  const size_t row = (size_t)a.Nqk * a.K, base = (size_t)b * a.T * row + (size_t)nq * a.K + 8 * g4;
-  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k;
-  auto at = [&](int tile) { return base + (size_t)min(t0 + 16 * tile + d, a.T - 1) * row; };
-  // forward: wave = tile of i, over j <= i, D[j][i];  backward: wave = tile of j, over i >= j, D[i][j]
-  const size_t own = at(wv);
-  for (int o = BWD ? wv : 0; o < (BWD ? 4 : wv + 1); ++o) {
-    const size_t other = at(o);
+  u2_t ph[4], pl[4];  // P's four columns (rows, transposed) per tile: an operand's halves as they are
+#pragma unroll
+  for (int o = 0; o < 4; ++o) ph[o] = pl[o] = u2_t{0u, 0u};
+  const int mine = 16 * wv + d;
+  auto tile = [&](int o, const u4_t *kt, const u4_t *qt) {
     f4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
-    for (int e = 0; e < a.K; e += 32) {
-      const u4_t ko = *(const u4_t *)(k + other + e), kw = *(const u4_t *)(k + own + e);
-      kk = mfma_bf16(ko, kw, kk);
-      if (BWD) qk = mfma_bf16(*(const u4_t *)(q + other + e), kw, qk);
-      else qk = mfma_bf16(ko, *(const u4_t *)(q + own + e), qk);
+#pragma unroll
+    for (int e = 0; e < KB; ++e) {
+      kk = mfma_bf16(kt[e], kw[e], kk);
+      qk = BWD ? mfma_bf16(qt[e], kw[e], qk) : mfma_bf16(kt[e], qw[e], qk);
     }
     settle(kk);
     settle(qk);
-    const int mine = 16 * wv + d;
     f4_t am, p;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -137,106 +162,121 @@ __global__ void __launch_bounds__(256) delta_half_prep_kernel(DeltaArgs a, int c
       const float e = exp2_((hi[i] - hi[j]) + (lo[i] - lo[j]));
       am[x] = j < i ? be[i] * e * kk[x] : 0.f;
       p[x] = j <= i ? e * qk[x] : 0.f;
+      if (BWD) As[i][j] = am[x];
+    }
+    if (!BWD) *(f4_t *)&As[mine][16 * o + 4 * g4] = am;
+    return p;
+  };
+#pragma unroll
+  for (int o = 0; o < 4; ++o) {
+    f4_t p = {0.f, 0.f, 0.f, 0.f};
+    if (o == wv) p = tile(o, kw, qw);
+    else if (BWD ? o > wv : o < wv) {
+      // (the register arrays are indexed by constants: one case per distance)
+      if constexpr (!BWD) {
+        if (o < 3) p = tile(o, ko[o < 3 ? o : 0], nullptr);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+          if (o - wv - 1 == x) p = tile(o, ko[x], qo[x]);
+      }
     }
     if (BWD) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) As[16 * o + 4 * g4 + x][mine] = am[x];
       const Pair4 s = split4(p);
-      *(u2_t *)&Ps[0][mine][16 * o + 4 * g4] = s.hi;
-      *(u2_t *)&Ps[BWD ? 1 : 0][mine][16 * o + 4 * g4] = s.lo;
+      ph[o] = s.hi;
+      pl[o] = s.lo;
     } else {
-      *(f4_t *)&As[mine][16 * o + 4 * g4] = am;
-      *(u2_t *)&Ps[0][mine][16 * o + 4 * g4] = pack4_h(p);
+      ph[o] = pack4_h(p);
     }
   }
   __syncthreads();
   if (lane < 16) {
     float x[16];
+    float *A0 = &As[16 * wv][16 * wv];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float s = d == i ? 1.f : 0.f;
+      float s[4] = {d == i ? 1.f : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < i; ++j) s = fmaf(-As[16 * wv + i][16 * wv + j], x[j], s);
-      x[i] = s;
-      Ts[16 * wv + i][16 * wv + d] = s;
+      for (int j = 0; j < i; ++j) s[j & 3] = fmaf(-A0[i * LA + j], x[j], s[j & 3]);
+      x[i] = (s[0] + s[1]) + (s[2] + s[3]);
     }
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) *(f4_t *)&Tt[16 * wv + d][16 * wv + i] = f4_t{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    for (int i = 0; i < 16; ++i) A0[i * LA + d] = x[i];
   }
   __syncthreads();
   const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+  // rows of an array as one factor, columns as the other
+  auto cols = [&](int r, int c) { return f4_t{As[r][c], As[r + 1][c], As[r + 2][c], As[r + 3][c]}; };
+  auto rows = [&](int r, int c) { return *(const f4_t *)&As[r][c]; };
+  auto put = [&](int r, int c, f4_t x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) As[r + i][c] = -x[i];
+  };
   if (wv < 2) {  // neighbours: block (2 wv + 1, 2 wv)
     const int r = 32 * wv + 16, c = 32 * wv;
-    f4_t x = mma_f32(&As[r + d][c + 4 * g4], &Tt[c + d][c + 4 * g4], zero);
+    f4_t x = mma_f32(rows(r + d, c + 4 * g4), cols(c + 4 * g4, c + d), zero);
     settle(x);
-    *(f4_t *)&Xt[16 * wv + d][4 * g4] = x;
-  }
-  __syncthreads();
-  if (wv < 2) {
-    const int r = 32 * wv + 16, c = 32 * wv;
-    f4_t x = mma_f32(&Ts[r + d][r + 4 * g4], &Xt[16 * wv + d][4 * g4], zero);
+    *(f4_t *)&Xt[16 * wv + d][4 * g4] = x;  // (read by this wave alone)
+    x = mma_f32(rows(r + d, r + 4 * g4), *(const f4_t *)&Xt[16 * wv + d][4 * g4], zero);
     settle(x);
-    x = -x;
-    *(f4_t *)&Tt[c + d][r + 4 * g4] = x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) Ts[r + 4 * g4 + i][c + d] = x[i];
+    put(r + 4 * g4, c + d, x);
   }
   __syncthreads();
   const int r = wv >> 1, c = wv & 1;  // tile (2 + r, c)
   {
-    f4_t x = zero;
-    if (c == 0) x = mma_f32(&As[32 + 16 * r + d][4 * g4], &Tt[d][4 * g4], x);
-    x = mma_f32(&As[32 + 16 * r + d][16 + 4 * g4], &Tt[16 * c + d][16 + 4 * g4], x);
+    f4_t x = mma_f32(rows(32 + 16 * r + d, 16 + 4 * g4), cols(16 + 4 * g4, 16 * c + d), zero);
+    if (c == 0) x = mma_f32(rows(32 + 16 * r + d, 4 * g4), cols(4 * g4, d), x);
     settle(x);
     *(f4_t *)&Xt[16 * c + d][16 * r + 4 * g4] = x;
   }
   __syncthreads();
   {
-    f4_t x = mma_f32(&Ts[32 + 16 * r + d][32 + 4 * g4], &Xt[16 * c + d][4 * g4], zero);
-    if (r == 1) x = mma_f32(&Ts[48 + d][48 + 4 * g4], &Xt[16 * c + d][16 + 4 * g4], x);
+    f4_t x = mma_f32(rows(32 + 16 * r + d, 32 + 4 * g4), *(const f4_t *)&Xt[16 * c + d][4 * g4], zero);
+    if (r == 1) x = mma_f32(rows(48 + d, 48 + 4 * g4), *(const f4_t *)&Xt[16 * c + d][16 + 4 * g4], x);
     settle(x);
-    x = -x;
-    *(f4_t *)&Tt[16 * c + d][32 + 16 * r + 4 * g4] = x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) Ts[32 + 16 * r + 4 * g4 + i][16 * c + d] = x[i];
+    put(32 + 16 * r + 4 * g4, 16 * c + d, x);
   }
   __syncthreads();
   half_t *Tm = mats + (size_t)blockIdx.x * 2 * kMat, *Pm = Tm + kMat;
-  const int me = 16 * wv + d;
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     if (BWD ? (kb == 0 && wv >= 2) : (kb == 1 && wv < 2)) continue;  // (zero)
-    const int c0 = 32 * kb + 8 * g4;
-    u4_t th, tl, ph, pl;
+    Pair4 t[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      f4_t x = *(const f4_t *)(BWD ? &Tt[me][c0 + 4 * u] : &Ts[me][c0 + 4 * u]);
-      u2_t y = *(const u2_t *)&Ps[0][me][c0 + 4 * u], z = *(const u2_t *)&Ps[BWD ? 1 : 0][me][c0 + 4 * u];
+      const int c0 = 32 * kb + 16 * u + 4 * g4;
+      f4_t x = BWD ? cols(c0, mine) : rows(mine, c0);
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int o = c0 + 4 * u + v;
-        if (BWD ? o < me : o > me) x[v] = 0.f;  // (tiles beyond the diagonal have not been written)
-      }
-      if (BWD ? c0 + 4 * u + 3 < me - d : c0 + 4 * u > me - d + 15) y = z = u2_t{0u, 0u};
-      const Pair4 s = split4(x);
-      th[2 * u] = s.hi.x; th[2 * u + 1] = s.hi.y;
-      tl[2 * u] = s.lo.x; tl[2 * u + 1] = s.lo.y;
-      ph[2 * u] = y.x; ph[2 * u + 1] = y.y;
-      pl[2 * u] = z.x; pl[2 * u + 1] = z.y;
+      for (int v = 0; v < 4; ++v)
+        if (BWD ? c0 + v < mine : c0 + v > mine) x[v] = 0.f;  // (tiles beyond the diagonal have not been written)
+      t[u] = split4(x);
     }
-    *(u4_t *)(Tm + mat_at(wv, kb, 0) + lane * 8) = th;
-    *(u4_t *)(Tm + mat_at(wv, kb, 1) + lane * 8) = tl;
-    *(u4_t *)(Pm + mat_at(wv, kb, 0) + lane * 8) = ph;
-    if (BWD) *(u4_t *)(Pm + mat_at(wv, kb, 1) + lane * 8) = pl;
+    auto join = [](u2_t x, u2_t y) { return u4_t{x.x, x.y, y.x, y.y}; };
+    *(u4_t *)(Tm + mat_at(wv, kb, 0) + lane * 8) = join(t[0].hi, t[1].hi);
+    *(u4_t *)(Tm + mat_at(wv, kb, 1) + lane * 8) = join(t[0].lo, t[1].lo);
+    *(u4_t *)(Pm + mat_at(wv, kb, 0) + lane * 8) = join(ph[2 * kb], ph[2 * kb + 1]);
+    if (BWD) *(u4_t *)(Pm + mat_at(wv, kb, 1) + lane * 8) = join(pl[2 * kb], pl[2 * kb + 1]);
   }
 }
 
-// ------------------------------------------------------------------ forward, chunks in order
-// Wave w has the chunk's steps 16 w .. 16 w + 15 in products over steps, and tiles w, w + 4, .. of the state.
+// ------------------------------------------------------------------ the kernels that run in order
+// A workgroup of four waves has VB columns of one state.  In products over steps wave w has the chunk's steps
+// 16 w .. 16 w + 15; of the state it has KTW row tiles times VTW column tiles, in fp32 registers throughout.
+//
+// What bounds them is the chain of a chunk: three products, each of which needs the one before from all waves.
+// So every operand of a product is read from LDS before its first instruction, what is off the chain (Q H, Q^T W,
+// results on their way out) lies in the shadow of such reads, and the next chunk's loads are in flight for a whole
+// chunk.  They are taken into the registers that use them before this chunk's results are stored: the counter that
+// a wait for loads looks at counts stores as well, in order.
 template <int K, int VB>
 struct Scan {
-  static constexpr int KB = K / 32, KT = K / 16, VT = VB / 16, NT = KT * VT, PW = (NT + 3) / 4;
+  static constexpr int KB = K / 32, KT = K / 16, VT = VB / 16;
+  static constexpr int KTW = KT >= 4 ? KT / 4 : 1, VTW = KT >= 4 ? VT : 1;
   static constexpr int LK = K + 8;
+  // row tile i and column tile j of wave w; with K = 32 two waves share a row tile (and with VB = 16 two have none)
+  static __device__ __forceinline__ int kt(int w, int i) { return KT >= 4 ? w + 4 * i : w % KT; }
+  static __device__ __forceinline__ int vt(int w, int j) { return KT >= 4 ? j : (w / KT) % VT; }
+  static __device__ __forceinline__ bool on(int w) { return KT >= 4 || w / KT < VT; }
 };
 // Where the operand that holds 16 rows x 32 columns of V goes: [V / 32][tiles][lane][8]; with VB = 16 a
 // workgroup has one half of the lanes.
@@ -251,227 +291,322 @@ __device__ __forceinline__ bool frag_at(int part, int tiles, int tile, size_t &o
     return lane < 32;
   }
 }
-// that operand, from an LDS array [VB][ld] whose columns c0 .. c0 + 15 are its rows
-template <int VB>
+// that operand, from an LDS array [VB][ld]: its rows are the columns c0 .. c0 + 15 (STEPS: c0 a tile of steps)
+template <int VB, bool STEPS>
 __device__ __forceinline__ h8_t frag_of(const half_t *base, int ld, int c0) {
   const int lane = threadIdx.x & 63, d = lane & 15, g = VB == 32 ? lane >> 4 : (lane >> 4) & 1;
-  const half_t *p = base + (8 * g + (d >> 2)) * ld + c0 + 4 * (d & 3);
+  const int c = STEPS ? 32 * (c0 >> 1) + 4 * (c0 & 1) + 8 * (d & 3) : c0 + 4 * (d & 3);
+  const half_t *p = base + (8 * g + (d >> 2)) * ld + c;
   return tr8(p, p + 4 * ld);
 }
+// Values that have arrived, in registers here and now (see above)
+template <typename X>
+__device__ __forceinline__ void pin(X &x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin8(h8_t &x) {
+  u4_t y = __builtin_bit_cast(u4_t, x);
+  pin(y);
+  x = __builtin_bit_cast(h8_t, y);
+}
+
+// A chunk's rows of q, k, v, dy, T, P: wave-uniform base and 32-bit offsets of the lanes (rows behind the last one
+// are the last one)
+template <int K, int VB>
+struct Chunk {
+  using S = Scan<K, VB>;
+  const char *q, *k, *v, *mats;
+  const float *gates;
+  size_t qstep, vstep;  // bytes of a chunk
+  uint32_t qrow, vrow;  // bytes of a row
+  int T;
+  __device__ __forceinline__ Chunk(const DeltaArgs &a, const void *vv, int unit, int part, int chunks,
+                                   const float *gts, const half_t *mts) {
+    const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
+    const size_t qr = (size_t)a.Nqk * K * 2, vr = (size_t)a.N * a.V * 2;
+    q = (const char *)a.q + (size_t)b * a.T * qr + (size_t)nq * K * 2;
+    k = (const char *)a.k + (size_t)b * a.T * qr + (size_t)nq * K * 2;
+    v = (const char *)vv + (size_t)b * a.T * vr + ((size_t)n * a.V + part * VB) * 2;
+    mats = (const char *)(mts + (size_t)unit * chunks * 2 * kMat);
+    gates = gts + (size_t)unit * chunks * kGates;
+    qstep = C * qr;
+    vstep = C * vr;
+    qrow = (uint32_t)qr;
+    vrow = (uint32_t)vr;
+    T = a.T;
+  }
+  __device__ __forceinline__ uint32_t at(int ch, int row, uint32_t stride) const {
+    return (uint32_t)min(row, T - 1 - ch * C) * stride;
+  }
+};
 
 template <int K, int VB>
 constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC) * 2; }
 
-template <int K, int VB>
+// Y: y is wanted;  CKPT: the chunks' states and U are
+template <int K, int VB, bool Y, bool CKPT>
 __global__ void __launch_bounds__(256, 2)
     delta_half_fwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const half_t *__restrict__ mats,
                           half_t *__restrict__ states, half_t *__restrict__ rows_u) {
   using S = Scan<K, VB>;
-  constexpr int KB = S::KB, KT = S::KT, VT = S::VT, NT = S::NT, PW = S::PW, LK = S::LK;
+  constexpr int KB = S::KB, KT = S::KT, VT = S::VT, KTW = S::KTW, VTW = S::VTW, LK = S::LK;
   extern __shared__ __align__(16) char lds[];
   half_t *ks = (half_t *)lds, *Ht = ks + C * LK, *Hl = Ht + VB * LK, *Rt = Hl + VB * LK, *Rl = Rt + VB * LC;
   half_t *Ut = Rl + VB * LC, *Wt = Ut + VB * LC, *Wl = Wt + VB * LC;
   int unit, part;
   if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
-  const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int d = lane & 15, g4 = lane >> 4;
-  const bool two = wv >= 2;  // (T and P are lower triangular: the first two waves have no steps above 31)
-  const size_t qrow = (size_t)a.Nqk * K, qbase = (size_t)b * a.T * qrow + (size_t)nq * K + 8 * g4;
-  const size_t vrow = (size_t)a.N * a.V, vbase = (size_t)b * a.T * vrow + (size_t)n * a.V + part * VB;
-  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k, *v = (const unsigned short *)a.v;
+  // T and P are lower triangular: the first two waves have no steps above 31, and zeros there (a branch around
+  // their products would not make the other two waves faster)
+  const bool two = wv >= 2;
+  const Chunk<K, VB> in(a, a.v, unit, part, chunks, gates, mats);
+  char *y0 = (char *)a.y + (in.v - (const char *)a.v);
   const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+  const size_t state0 = (size_t)unit * K * a.V + part * VB + d;  // element (0, d) of my columns
 
-  f4_t H[PW];
+  f4_t H[KTW][VTW];
 #pragma unroll
-  for (int p = 0; p < PW; ++p) {
-    const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-    H[p] = zero;
-    if (a.H0 && t < NT)
+  for (int i = 0; i < KTW; ++i)
+#pragma unroll
+    for (int j = 0; j < VTW; ++j)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        H[p][x] = a.H0[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d];
-  }
-  u4_t nk[KB], nqr[KB], nT[4], nP[2];
+        H[i][j][x] = a.H0 ? a.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
+  u4_t nk[KB], nq[KB], nT[4], nP[2];
   unsigned short nv[VT][4];
   f4_t nge, ngl, nbe;
   float ng1, ngc;
   auto fetch = [&](int ch) {
-    const int t0 = ch * C;
-    const size_t at = (size_t)unit * chunks + ch, r = qbase + (size_t)min(t0 + 16 * wv + d, a.T - 1) * qrow;
-#pragma unroll
-    for (int i = 0; i < KB; ++i) {
-      nk[i] = *(const u4_t *)(k + r + 32 * i);
-      nqr[i] = *(const u4_t *)(q + r + 32 * i);
-    }
-    const half_t *Tm = mats + at * 2 * kMat + lane * 8, *Pm = Tm + kMat;
-    nT[0] = *(const u4_t *)(Tm + mat_at(wv, 0, 0));
-    nT[1] = *(const u4_t *)(Tm + mat_at(wv, 0, 1));
-    nP[0] = *(const u4_t *)(Pm + mat_at(wv, 0, 0));
+    const char *k = in.k + ch * in.qstep, *q = in.q + ch * in.qstep, *v = in.v + ch * in.vstep;
+    const char *m = in.mats + (size_t)ch * 4 * kMat;
+    const float *gt = in.gates + (size_t)ch * kGates;
+    const uint32_t r = in.at(ch, 16 * wv + d, in.qrow) + 16 * g4;
     const int kb = two ? 1 : 0;  // (unconditional: the first two waves read their only block again)
-    nT[2] = *(const u4_t *)(Tm + mat_at(wv, kb, 0));
-    nT[3] = *(const u4_t *)(Tm + mat_at(wv, kb, 1));
-    nP[1] = *(const u4_t *)(Pm + mat_at(wv, kb, 0));
+#pragma unroll
+    for (int i = 0; i < KB; ++i) nk[i] = *(const u4_t *)(k + (r + 64 * i));
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const size_t rv = vbase + (size_t)min(t0 + 16 * wv + 4 * g4 + x, a.T - 1) * vrow + d;
+      const uint32_t rv = in.at(ch, 16 * wv + 4 * g4 + x, in.vrow) + 2 * d;
 #pragma unroll
-      for (int t = 0; t < VT; ++t) nv[t][x] = v[rv + 16 * t];
+      for (int t = 0; t < VT; ++t) nv[t][x] = *(const unsigned short *)(v + (rv + 32 * t));
     }
-    const float *gt = gates + at * kGates + 16 * wv;
-    nge = *(const f4_t *)(gt + 4 * g4);
-    ngl = *(const f4_t *)(gt + C + 4 * g4);
-    nbe = *(const f4_t *)(gt + 4 * C + 4 * g4);
-    ng1 = gt[d];
-    ngc = gates[at * kGates + C - 1];
-  };
-  auto put_state = [&]() {
+    nge = *(const f4_t *)(gt + 16 * wv + 4 * g4);
+    nbe = *(const f4_t *)(gt + 4 * C + 16 * wv + 4 * g4);
+    ngl = *(const f4_t *)(gt + C + 16 * wv + 4 * g4);
+    ng1 = gt[16 * wv + d];
+    ngc = gt[C - 1];
 #pragma unroll
-    for (int p = 0; p < PW; ++p) {
-      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-      if (t < NT) {
-        const Pair4 s = split4(H[p]);
-        *(u2_t *)&Ht[(16 * vt + d) * LK + 16 * kt + 4 * g4] = s.hi;
-        *(u2_t *)&Hl[(16 * vt + d) * LK + 16 * kt + 4 * g4] = s.lo;
-      }
+    for (int i = 0; i < 2; ++i) {
+      nT[i] = *(const u4_t *)(m + 2 * mat_at(wv, 0, i) + 16 * lane);
+      nT[2 + i] = *(const u4_t *)(m + 2 * mat_at(wv, kb, i) + 16 * lane);
+    }
+    if (Y) {
+      nP[0] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, 0, 0) + 16 * lane);
+      nP[1] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, kb, 0) + 16 * lane);
+#pragma unroll
+      for (int i = 0; i < KB; ++i) nq[i] = *(const u4_t *)(q + (r + 64 * i));
     }
   };
-  put_state();
-  if (chunks > 0) fetch(0);
-  for (int ch = 0; ch < chunks; ++ch) {
-    const int t0 = ch * C;
-    const size_t at = (size_t)unit * chunks + ch;
-    h8_t kf[KB], qf[KB], Tf[4], Pf[2];
-    f4_t vf[VT];
+  h8_t kf[KB], qf[KB], Tf[4], Pf[2];
+  f4_t vf[VT], ge, gl, be;
+  float g1, gc;
+  auto take = [&]() {
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
       kf[i] = bf16_to_h8(nk[i]);
-      qf[i] = bf16_to_h8(nqr[i]);
+      pin8(kf[i]);
+      if (Y) {
+        qf[i] = bf16_to_h8(nq[i]);
+        pin8(qf[i]);
+      }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) Tf[i] = __builtin_bit_cast(h8_t, nT[i]);
+    for (int i = 0; i < 4; ++i) {
+      pin(nT[i]);
+      Tf[i] = __builtin_bit_cast(h8_t, i < 2 || two ? nT[i] : u4_t{0u, 0u, 0u, 0u});
+    }
+    if (Y)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) Pf[i] = __builtin_bit_cast(h8_t, nP[i]);
+      for (int i = 0; i < 2; ++i) {
+        pin(nP[i]);
+        Pf[i] = __builtin_bit_cast(h8_t, i < 1 || two ? nP[i] : u4_t{0u, 0u, 0u, 0u});
+      }
 #pragma unroll
-    for (int t = 0; t < VT; ++t)
+    for (int t = 0; t < VT; ++t) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) vf[t][x] = bf16_bits_to_f32(nv[t][x]);
-    const f4_t ge = nge, gl = ngl, be = nbe;
-    const float g1 = ng1, gc = ngc;
+      pin(vf[t]);
+    }
+    ge = nge; gl = ngl; be = nbe; g1 = ng1; gc = ngc;
+    pin(ge); pin(gl); pin(be); pin(g1); pin(gc);
+  };
+  auto put_state = [&]() {
+    if (S::on(wv))
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          const Pair4 s = split4(H[i][j]);
+          const int o = (16 * S::vt(wv, j) + d) * LK + 16 * S::kt(wv, i) + 4 * g4;
+          *(u2_t *)&Ht[o] = s.hi;
+          *(u2_t *)&Hl[o] = s.lo;
+        }
+  };
+  put_state();
+  if (chunks > 0) {
+    fetch(0);
+    take();
+  }
+  const int w = place(wv);
+  for (int ch = 0; ch < chunks; ++ch) {
     lds_barrier();  // the state is there, and k of the chunk before has been read
+    // R = beta (v - e^G K H): D[step][column]
+    h8_t hh[VT][KB], hl[VT][KB];
+#pragma unroll
+    for (int i = 0; i < KB; ++i)
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
+        hh[t][i] = ld8(Ht + o);
+        hl[t][i] = ld8(Hl + o);
+      }
     fetch(min(ch + 1, chunks - 1));
 #pragma unroll
     for (int i = 0; i < KB; ++i) *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
-    // R = beta (v - e^G K H): D[step][column]
+    f4_t x[VT], xl[VT];
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      f4_t x = zero;
+    for (int t = 0; t < VT; ++t) x[t] = xl[t] = zero;
 #pragma unroll
-      for (int i = 0; i < KB; ++i) {
-        const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
-        x = mfma_k32(kf[i], ld8(Ht + o), x);
-        x = mfma_k32(kf[i], ld8(Hl + o), x);
-      }
-      settle(x);
-      const Pair4 s = split4(be * (vf[t] - ge * x));
-      *(u2_t *)&Rt[(16 * t + d) * LC + 16 * wv + 4 * g4] = s.hi;
-      *(u2_t *)&Rl[(16 * t + d) * LC + 16 * wv + 4 * g4] = s.lo;
-    }
-    if (states) {
-      for (int kt = wv; kt < KT; kt += 4) {
-        size_t o;
-        const h8_t f = frag_of<VB>(Ht, LK, 16 * kt);
-        if (frag_at<VB>(part, KT, kt, o)) *(h8_t *)(states + at * K * a.V + o) = f;
-      }
-    }
-    lds_barrier();
-    // (Q H)^T: D[column][step], off the chain
-    f4_t y[VT];
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      y[t] = zero;
-      if (a.write_y)
-#pragma unroll
-        for (int i = 0; i < KB; ++i) y[t] = mfma_k32(ld8(Ht + (16 * t + d) * LK + 32 * i + 8 * g4), qf[i], y[t]);
-      settle(y[t]);
-    }
-    // U = T R: D[step][column]
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      const int o = (16 * t + d) * LC + 8 * g4;
-      f4_t u = zero;
-      {
-        const h8_t rh = ld8(Rt + o), rl = ld8(Rl + o);
-        u = mfma_k32(Tf[0], rh, u);
-        u = mfma_k32(Tf[1], rh, u);
-        u = mfma_k32(Tf[0], rl, u);
-      }
-      if (two) {
-        const h8_t rh = ld8(Rt + o + 32), rl = ld8(Rl + o + 32);
-        u = mfma_k32(Tf[2], rh, u);
-        u = mfma_k32(Tf[3], rh, u);
-        u = mfma_k32(Tf[2], rl, u);
-      }
-      settle(u);
-      const int w = (16 * t + d) * LC + 16 * wv + 4 * g4;
-      *(u2_t *)&Ut[w] = pack4_h(u);
-      const Pair4 s = split4(gl * u);
-      *(u2_t *)&Wt[w] = s.hi;
-      *(u2_t *)&Wl[w] = s.lo;
-    }
-    lds_barrier();
-    // H = e^{G_C} H + K^T W: D[row][column]
-#pragma unroll
-    for (int p = 0; p < PW; ++p) {
-      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-      if (t < NT) {
-        f4_t x = gc * H[p];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const h8_t kT = ld8_tr(ks, LK, 32 * kb, 16 * kt);
-          const int o = (16 * vt + d) * LC + 32 * kb + 8 * g4;
-          x = mfma_k32(kT, ld8(Wt + o), x);
-          x = mfma_k32(kT, ld8(Wl + o), x);
-        }
-        settle(x);
-        H[p] = x;
-      }
-    }
-    put_state();
-    // y = e^G (Q H)^T + (P U)^T, and U for the backward
-    if (a.write_y) {
-      const int step = t0 + 16 * wv + d;
+    for (int i = 0; i < KB; ++i)
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
-        const int o = (16 * t + d) * LC + 8 * g4;
-        f4_t x = mfma_k32(ld8(Ut + o), Pf[0], g1 * y[t]);
-        if (two) x = mfma_k32(ld8(Ut + o + 32), Pf[1], x);
-        settle(x);
-        if (step < a.T)
-          *(u2_t *)((unsigned short *)a.y + vbase + (size_t)step * vrow + 16 * t + 4 * g4) =
-              u2_t{pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])};
+        x[t] = mfma_k32(kf[i], hh[t][i], x[t]);
+        xl[t] = mfma_k32(kf[i], hl[t][i], xl[t]);
       }
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      const Pair4 s = split4(be * (vf[t] - ge * (x[t] + xl[t])));
+      *(u2_t *)&Rt[(16 * t + d) * LC + w] = s.hi;
+      *(u2_t *)&Rl[(16 * t + d) * LC + w] = s.lo;
     }
-    if (rows_u) {
+    lds_barrier();
+    // U = T R: D[step][column];  off the chain (Q H)^T: D[column][step]
+    h8_t rh[VT][2], rl[VT][2], hs[KTW], kT[KTW][2];
+    f4_t y[VT], u[VT], ul[VT];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        const int o = (16 * t + d) * LC + 32 * kb + 8 * g4;
+        rh[t][kb] = ld8(Rt + o);
+        rl[t][kb] = ld8(Rl + o);
+      }
+    if (CKPT)
+#pragma unroll
+      for (int i = 0; i < KTW; ++i) hs[i] = frag_of<VB, false>(Ht, LK, 16 * S::kt(wv, i));
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) kT[i][kb] = ld8_steps(ks, LK, 32 * kb, 16 * S::kt(wv, i));
+#pragma unroll
+    for (int t = 0; t < VT; ++t) y[t] = u[t] = ul[t] = zero;
+    if (Y)
+#pragma unroll
+      for (int i = 0; i < KB; ++i)
+#pragma unroll
+        for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf[i], y[t]);
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      u[t] = mfma_k32(Tf[0], rh[t][0], u[t]);
+      ul[t] = mfma_k32(Tf[1], rh[t][0], ul[t]);
+      ul[t] = mfma_k32(Tf[0], rl[t][0], ul[t]);
+      u[t] = mfma_k32(Tf[2], rh[t][1], u[t]);
+      ul[t] = mfma_k32(Tf[3], rh[t][1], ul[t]);
+      ul[t] = mfma_k32(Tf[2], rl[t][1], ul[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      settle(u[t]);
+      settle(ul[t]);
+      const f4_t uu = u[t] + ul[t];
+      const Pair4 s = split4(gl * uu);
+      *(u2_t *)&Wt[(16 * t + d) * LC + w] = s.hi;
+      *(u2_t *)&Wl[(16 * t + d) * LC + w] = s.lo;
+      *(u2_t *)&Ut[(16 * t + d) * LC + w] = pack4_h(uu);
+    }
+    lds_barrier();
+    // H = e^{G_C} H + K^T W: D[row][column];  y = e^G (Q H)^T + (P U)^T
+    h8_t wh[VTW][2], wl[VTW][2], uf[VT][2], us;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) {
+        const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
+        wh[j][kb] = ld8(Wt + o);
+        wl[j][kb] = ld8(Wl + o);
+      }
+    if (Y)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int t = 0; t < VT; ++t) uf[t][kb] = ld8(Ut + (16 * t + d) * LC + 32 * kb + 8 * g4);
+    if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) H[i][j] *= gc;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          H[i][j] = mfma_k32(kT[i][kb], wl[j][kb], H[i][j]);
+          H[i][j] = mfma_k32(kT[i][kb], wh[j][kb], H[i][j]);
+        }
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) settle(H[i][j]);
+    put_state();
+    if (Y) {
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        y[t] = mfma_k32(uf[t][0], Pf[0], g1 * y[t]);
+        y[t] = mfma_k32(uf[t][1], Pf[1], y[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < VT; ++t) settle(y[t]);
+    }
+    take();
+    if (Y && ch * C + 16 * wv + d < a.T) {
+      char *o = y0 + ch * in.vstep + (uint32_t)(16 * wv + d) * in.vrow + 8 * g4;
+#pragma unroll
+      for (int t = 0; t < VT; ++t)
+        *(u2_t *)(o + 32 * t) = u2_t{pack2_bf16(y[t][0], y[t][1]), pack2_bf16(y[t][2], y[t][3])};
+    }
+    if (CKPT) {
+      const size_t at = (size_t)unit * chunks + ch;
       size_t o;
-      const h8_t f = frag_of<VB>(Ut, LC, 16 * wv);
-      if (frag_at<VB>(part, 4, wv, o)) *(h8_t *)(rows_u + at * C * a.V + o) = f;
+      if (KT >= 4 || wv < KT)
+#pragma unroll
+        for (int i = 0; i < KTW; ++i)
+          if (frag_at<VB>(part, KT, S::kt(wv, i), o)) *(h8_t *)(states + at * K * a.V + o) = hs[i];
+      if (frag_at<VB>(part, 4, wv, o)) *(h8_t *)(rows_u + at * C * a.V + o) = us;
     }
   }
-  if (a.HT)
+  if (a.HT && S::on(wv))
 #pragma unroll
-    for (int p = 0; p < PW; ++p) {
-      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-      if (t < NT)
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          a.HT[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d] = H[p][x];
-    }
+          a.HT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] = H[i][j][x];
 }
 
-// ------------------------------------------------------------------ backward, chunks in reverse order
-// Gradients of a chunk are brought near one by s, a power of two from the largest |dH| and |dy| of the
-// workgroup's columns: with unit keys nothing below exceeds some hundreds then, and the pairs' 2^-25 is small.
+// Backward, chunks in reverse order.  Gradients of a chunk are brought near one by s, a power of two from the
+// largest |dH| and |dy| of the workgroup's columns: with unit keys nothing below exceeds some hundreds then, and
+// the pairs' 2^-25 is small.
 template <int K, int VB>
 constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC) * 2 + 16; }
 
@@ -480,7 +615,7 @@ __global__ void __launch_bounds__(256, 2)
     delta_half_bwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const half_t *__restrict__ mats,
                           half_t *__restrict__ dstates, half_t *__restrict__ rows_z, float *__restrict__ scales) {
   using S = Scan<K, VB>;
-  constexpr int KB = S::KB, KT = S::KT, VT = S::VT, NT = S::NT, PW = S::PW, LK = S::LK;
+  constexpr int KB = S::KB, KT = S::KT, VT = S::VT, KTW = S::KTW, VTW = S::VTW, LK = S::LK;
   extern __shared__ __align__(16) char lds[];
   half_t *ks = (half_t *)lds, *qs = ks + C * LK, *Ht = qs + C * LK, *Hl = Ht + VB * LK, *Yt = Hl + VB * LK;
   half_t *Wt = Yt + VB * LC, *Wl = Wt + VB * LC, *Ut = Wl + VB * LC, *Ul = Ut + VB * LC;
@@ -488,110 +623,126 @@ __global__ void __launch_bounds__(256, 2)
   float *red = (float *)(Ul + VB * LC);
   int unit, part;
   if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
-  const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int d = lane & 15, g4 = lane >> 4;
   const bool two = wv < 2;  // (transposed: the last two waves have no steps below 32)
-  const size_t qrow = (size_t)a.Nqk * K, qbase = (size_t)b * a.T * qrow + (size_t)nq * K + 8 * g4;
-  const size_t vrow = (size_t)a.N * a.V, vbase = (size_t)b * a.T * vrow + (size_t)n * a.V + part * VB;
-  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k;
-  const unsigned short *dy = (const unsigned short *)a.dy;
+  const Chunk<K, VB> in(a, a.dy, unit, part, chunks, gates, mats);
+  char *dv0 = (char *)a.dv + (in.v - (const char *)a.dy);
   const f4_t zero = {0.f, 0.f, 0.f, 0.f};
+  const size_t state0 = (size_t)unit * K * a.V + part * VB + d;
 
-  f4_t D[PW];
+  f4_t D[KTW][VTW];
 #pragma unroll
-  for (int p = 0; p < PW; ++p) {
-    const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-    D[p] = zero;
-    if (a.dHT && t < NT)
+  for (int i = 0; i < KTW; ++i)
+#pragma unroll
+    for (int j = 0; j < VTW; ++j)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        D[p][x] = a.dHT[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d];
-  }
-  u4_t nk[KB], nqr[KB], nT[4], nP[4];
+        D[i][j][x] = a.dHT ? a.dHT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
+  u4_t nk[KB], nq[KB], nT[4], nP[4];
   unsigned short ny[VT][4];
   f4_t nge, ngl, nbe;
   float nb1, ngc, nom;
   auto fetch = [&](int ch) {
-    const int t0 = ch * C;
-    const size_t at = (size_t)unit * chunks + ch, r = qbase + (size_t)min(t0 + 16 * wv + d, a.T - 1) * qrow;
-#pragma unroll
-    for (int i = 0; i < KB; ++i) {
-      nk[i] = *(const u4_t *)(k + r + 32 * i);
-      nqr[i] = *(const u4_t *)(q + r + 32 * i);
-    }
-    const half_t *Tm = mats + at * 2 * kMat + lane * 8, *Pm = Tm + kMat;
+    const char *k = in.k + ch * in.qstep, *q = in.q + ch * in.qstep, *y = in.v + ch * in.vstep;
+    const char *m = in.mats + (size_t)ch * 4 * kMat;
+    const float *gt = in.gates + (size_t)ch * kGates;
+    const uint32_t r = in.at(ch, 16 * wv + d, in.qrow) + 16 * g4;
     const int kb = two ? 0 : 1;  // (unconditional: the last two waves read their only block again)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      nT[i] = *(const u4_t *)(Tm + mat_at(wv, 1, i));
-      nP[i] = *(const u4_t *)(Pm + mat_at(wv, 1, i));
-      nT[2 + i] = *(const u4_t *)(Tm + mat_at(wv, kb, i));
-      nP[2 + i] = *(const u4_t *)(Pm + mat_at(wv, kb, i));
-    }
-#pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const size_t rv = vbase + (size_t)min(t0 + 16 * wv + 4 * g4 + x, a.T - 1) * vrow + d;
+      const uint32_t rv = in.at(ch, 16 * wv + 4 * g4 + x, in.vrow) + 2 * d;
 #pragma unroll
-      for (int t = 0; t < VT; ++t) ny[t][x] = dy[rv + 16 * t];
+      for (int t = 0; t < VT; ++t) ny[t][x] = *(const unsigned short *)(y + (rv + 32 * t));
     }
-    const float *gt = gates + at * kGates + 16 * wv;
-    nge = *(const f4_t *)(gt + 4 * g4);
-    ngl = *(const f4_t *)(gt + C + 4 * g4);
-    nbe = *(const f4_t *)(gt + 4 * C + 4 * g4);
-    nb1 = gt[4 * C + d];
-    nom = gate_unit(gates[at * kGates + 2 * C]);
-    ngc = nom * gates[at * kGates + C - 1];
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      nk[i] = *(const u4_t *)(k + (r + 64 * i));
+      nq[i] = *(const u4_t *)(q + (r + 64 * i));
+    }
+    nge = *(const f4_t *)(gt + 16 * wv + 4 * g4);
+    ngl = *(const f4_t *)(gt + C + 16 * wv + 4 * g4);
+    nbe = *(const f4_t *)(gt + 4 * C + 16 * wv + 4 * g4);
+    nb1 = gt[4 * C + 16 * wv + d];
+    nom = gt[2 * C];
+    ngc = gt[C - 1];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      nT[i] = *(const u4_t *)(m + 2 * mat_at(wv, 1, i) + 16 * lane);
+      nT[2 + i] = *(const u4_t *)(m + 2 * mat_at(wv, kb, i) + 16 * lane);
+      nP[i] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, 1, i) + 16 * lane);
+      nP[2 + i] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, kb, i) + 16 * lane);
+    }
   };
-  if (chunks > 0) fetch(chunks - 1);
+  h8_t kf[KB], qf[KB], Tf[4], Pf[4];
+  f4_t yf[VT], ge, gl, be;
+  float b1, gc, om;
+  auto take = [&](int ch) {
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) yf[t][x] = ch * C + 16 * wv + 4 * g4 + x < a.T ? bf16_bits_to_f32(ny[t][x]) : 0.f;
+      pin(yf[t]);
+    }
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      kf[i] = bf16_to_h8(nk[i]);
+      qf[i] = bf16_to_h8(nq[i]);
+      pin8(kf[i]);
+      pin8(qf[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pin(nT[i]);
+      pin(nP[i]);
+      Tf[i] = __builtin_bit_cast(h8_t, i < 2 || two ? nT[i] : u4_t{0u, 0u, 0u, 0u});
+      Pf[i] = __builtin_bit_cast(h8_t, i < 2 || two ? nP[i] : u4_t{0u, 0u, 0u, 0u});
+    }
+    ge = nge; gl = ngl; be = nbe; b1 = nb1; om = gate_unit(nom); gc = om * ngc;
+    pin(ge); pin(gl); pin(be); pin(b1); pin(gc); pin(om);
+  };
+  if (chunks > 0) {
+    fetch(chunks - 1);
+    take(chunks - 1);
+  }
+  const int w = place(wv);
   for (int ch = chunks - 1; ch >= 0; --ch) {
-    const int t0 = ch * C;
-    const size_t at = (size_t)unit * chunks + ch;
-    h8_t kf[KB], Tf[4], Pf[4];
-    f4_t yf[VT];
     float top = 0.f;
 #pragma unroll
     for (int t = 0; t < VT; ++t)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        yf[t][x] = t0 + 16 * wv + 4 * g4 + x < a.T ? bf16_bits_to_f32(ny[t][x]) : 0.f;
-        top = fmaxf(top, fabsf(yf[t][x]));
-      }
+      for (int x = 0; x < 4; ++x) top = fmaxf(top, fabsf(yf[t][x]));
 #pragma unroll
-    for (int p = 0; p < PW; ++p)
+    for (int i = 0; i < KTW; ++i)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) top = fmaxf(top, fabsf(D[p][x]));
+      for (int j = 0; j < VTW; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top = fmaxf(top, fabsf(D[i][j][x]));
     top = group_max_nonneg<64>(top);
     if (lane == 0) red[wv] = top;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      Tf[i] = __builtin_bit_cast(h8_t, nT[i]);
-      Pf[i] = __builtin_bit_cast(h8_t, nP[i]);
-    }
-    const f4_t ge = nge, gl = ngl, be = nbe;
-    const float b1 = nb1, gc = ngc, om = nom;
     lds_barrier();  // (and everything of the chunk before has been read)
-    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const int e = min(max(ilog2f(top), -100), 100);
-    const float s = pow2i(-e), inv = pow2i(e);
+    const f4_t tops = *(const f4_t *)red;
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
-      kf[i] = bf16_to_h8(nk[i]);
       *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
-      *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = bf16_to_h8(nqr[i]);
+      *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = qf[i];
     }
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const int e = min(max(ilog2f(top), -100), 100);
+    const float s = pow2i(-e), inv = pow2i(e);
+    if (S::on(wv))
 #pragma unroll
-    for (int p = 0; p < PW; ++p) {
-      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-      if (t < NT) {
-        const Pair4 x = split4(s * D[p]);
-        *(u2_t *)&Ht[(16 * vt + d) * LK + 16 * kt + 4 * g4] = x.hi;
-        *(u2_t *)&Hl[(16 * vt + d) * LK + 16 * kt + 4 * g4] = x.lo;
-      }
-    }
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          const Pair4 x = split4(s * D[i][j]);
+          const int o = (16 * S::vt(wv, j) + d) * LK + 16 * S::kt(wv, i) + 4 * g4;
+          *(u2_t *)&Ht[o] = x.hi;
+          *(u2_t *)&Hl[o] = x.lo;
+        }
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
-      const int o = (16 * t + d) * LC + 16 * wv + 4 * g4;
+      const int o = (16 * t + d) * LC + w;
       const f4_t y = s * yf[t];
       const Pair4 x = split4(ge * y);
       *(u2_t *)&Yt[o] = pack4_h(y);
@@ -599,130 +750,173 @@ __global__ void __launch_bounds__(256, 2)
       *(u2_t *)&Wl[o] = x.lo;
     }
     lds_barrier();
-    fetch(max(ch - 1, 0));
     // dU = P^T dY + e^{G_C - G} K dH: D[step][column]
+    h8_t hh[VT][KB], hl[VT][KB], yy[VT][2];
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      f4_t u = zero;
+    for (int i = 0; i < KB; ++i)
 #pragma unroll
-      for (int i = 0; i < KB; ++i) {
+      for (int t = 0; t < VT; ++t) {
         const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
-        u = mfma_k32(kf[i], ld8(Ht + o), u);
-        u = mfma_k32(kf[i], ld8(Hl + o), u);
+        hh[t][i] = ld8(Ht + o);
+        hl[t][i] = ld8(Hl + o);
       }
-      settle(u);
-      u = gl * u;
-      const int o = (16 * t + d) * LC + 8 * g4;
-      {
-        const h8_t y = ld8(Yt + o + 32);
-        u = mfma_k32(Pf[0], y, u);
-        u = mfma_k32(Pf[1], y, u);
-      }
-      if (two) {
-        const h8_t y = ld8(Yt + o);
-        u = mfma_k32(Pf[2], y, u);
-        u = mfma_k32(Pf[3], y, u);
-      }
-      settle(u);
-      const Pair4 x = split4(u);
-      const int w = (16 * t + d) * LC + 16 * wv + 4 * g4;
-      *(u2_t *)&Ut[w] = x.hi;
-      *(u2_t *)&Ul[w] = x.lo;
-    }
-    // Q^T e^G dY, off the chain
-    f4_t acc[PW];
 #pragma unroll
-    for (int p = 0; p < PW; ++p) {
-      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-      acc[p] = zero;
-      if (t < NT) {
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const h8_t qT = ld8_tr(qs, LK, 32 * kb, 16 * kt);
-          const int o = (16 * vt + d) * LC + 32 * kb + 8 * g4;
-          acc[p] = mfma_k32(qT, ld8(Wt + o), acc[p]);
-          acc[p] = mfma_k32(qT, ld8(Wl + o), acc[p]);
-        }
-        settle(acc[p]);
+      for (int t = 0; t < VT; ++t) yy[t][kb] = ld8(Yt + (16 * t + d) * LC + 32 * kb + 8 * g4);
+    fetch(max(ch - 1, 0));
+    f4_t u[VT], ul[VT], py[VT];
+#pragma unroll
+    for (int t = 0; t < VT; ++t) u[t] = ul[t] = py[t] = zero;
+#pragma unroll
+    for (int i = 0; i < KB; ++i)
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        u[t] = mfma_k32(kf[i], hh[t][i], u[t]);
+        ul[t] = mfma_k32(kf[i], hl[t][i], ul[t]);
       }
-    }
-    for (int kt = wv; kt < KT; kt += 4) {
-      size_t o;
-      const h8_t f = frag_of<VB>(Ht, LK, 16 * kt);
-      if (frag_at<VB>(part, KT, kt, o)) *(h8_t *)(dstates + at * K * a.V + o) = f;
-    }
-    if (threadIdx.x == 0) scales[at * (a.V / VB) + part] = s;
-    lds_barrier();
-    // Z = T^T dU, as D[step][column] for the state and as D[column][step] for what is written
-    f4_t z[VT];
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
-      const int o = (16 * t + d) * LC + 8 * g4;
-      f4_t x = zero;
-      z[t] = zero;
-      {
-        const h8_t uh = ld8(Ut + o + 32), ul = ld8(Ul + o + 32);
-        x = mfma_k32(Tf[0], uh, x);
-        x = mfma_k32(Tf[1], uh, x);
-        x = mfma_k32(Tf[0], ul, x);
-        z[t] = mfma_k32(uh, Tf[0], z[t]);
-        z[t] = mfma_k32(uh, Tf[1], z[t]);
-        z[t] = mfma_k32(ul, Tf[0], z[t]);
-      }
-      if (two) {
-        const h8_t uh = ld8(Ut + o), ul = ld8(Ul + o);
-        x = mfma_k32(Tf[2], uh, x);
-        x = mfma_k32(Tf[3], uh, x);
-        x = mfma_k32(Tf[2], ul, x);
-        z[t] = mfma_k32(uh, Tf[2], z[t]);
-        z[t] = mfma_k32(uh, Tf[3], z[t]);
-        z[t] = mfma_k32(ul, Tf[2], z[t]);
-      }
-      settle(x);
-      settle(z[t]);
-      const Pair4 w = split4(-(be * ge) * x);
-      const int o2 = (16 * t + d) * LC + 16 * wv + 4 * g4;
-      *(u2_t *)&Zt[o2] = w.hi;
-      *(u2_t *)&Zl[o2] = w.lo;
+      py[t] = mfma_k32(Pf[0], yy[t][1], py[t]);
+      py[t] = mfma_k32(Pf[1], yy[t][1], py[t]);
+      py[t] = mfma_k32(Pf[2], yy[t][0], py[t]);
+      py[t] = mfma_k32(Pf[3], yy[t][0], py[t]);
     }
-    lds_barrier();
 #pragma unroll
-    for (int p = 0; p < PW; ++p) {
-      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-      if (t < NT) {
+    for (int t = 0; t < VT; ++t) {
+      settle(u[t]);
+      settle(ul[t]);
+      settle(py[t]);
+      const Pair4 x = split4(gl * (u[t] + ul[t]) + py[t]);
+      *(u2_t *)&Ut[(16 * t + d) * LC + w] = x.hi;
+      *(u2_t *)&Ul[(16 * t + d) * LC + w] = x.lo;
+    }
+    // (what Q^T e^G dY needs, before Z takes W's place)
+    h8_t hs[KTW], xT[KTW][2], wh[VTW][2], wl[VTW][2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) {
+        const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
+        wh[j][kb] = ld8(Wt + o);
+        wl[j][kb] = ld8(Wl + o);
+      }
+#pragma unroll
+      for (int i = 0; i < KTW; ++i) xT[i][kb] = ld8_steps(qs, LK, 32 * kb, 16 * S::kt(wv, i));
+    }
+#pragma unroll
+    for (int i = 0; i < KTW; ++i) hs[i] = frag_of<VB, false>(Ht, LK, 16 * S::kt(wv, i));
+    lds_barrier();
+    // Z = T^T dU as D[step][column] for the state, and as D[column][step] for what is written
+    h8_t uh[VT][2], uo[VT][2];
+#pragma unroll
+    for (int kb = 1; kb >= 0; --kb)
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        const int o = (16 * t + d) * LC + 32 * kb + 8 * g4;
+        uh[t][kb] = ld8(Ut + o);
+        uo[t][kb] = ld8(Ul + o);
+      }
+    f4_t acc[KTW][VTW];
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) {
+        acc[i][j] = zero;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-          const h8_t kT = ld8_tr(ks, LK, 32 * kb, 16 * kt);
-          const int o = (16 * vt + d) * LC + 32 * kb + 8 * g4;
-          acc[p] = mfma_k32(kT, ld8(Zt + o), acc[p]);
-          acc[p] = mfma_k32(kT, ld8(Zl + o), acc[p]);
+          acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], acc[i][j]);
+          acc[i][j] = mfma_k32(xT[i][kb], wh[j][kb], acc[i][j]);
         }
-        settle(acc[p]);
-        D[p] = gc * D[p] + (inv * om) * acc[p];
       }
+    f4_t x[VT], xl[VT], z[VT];
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      x[t] = mfma_k32(Tf[0], uh[t][1], zero);
+      xl[t] = mfma_k32(Tf[1], uh[t][1], zero);
+      xl[t] = mfma_k32(Tf[0], uo[t][1], xl[t]);
+      x[t] = mfma_k32(Tf[2], uh[t][0], x[t]);
+      xl[t] = mfma_k32(Tf[3], uh[t][0], xl[t]);
+      xl[t] = mfma_k32(Tf[2], uo[t][0], xl[t]);
     }
-    const int step = t0 + 16 * wv + d;
+    const f4_t bg = -(be * ge);
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      settle(x[t]);
+      settle(xl[t]);
+      const Pair4 y = split4(bg * (x[t] + xl[t]));
+      *(u2_t *)&Zt[(16 * t + d) * LC + w] = y.hi;
+      *(u2_t *)&Zl[(16 * t + d) * LC + w] = y.lo;
+    }
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) xT[i][kb] = ld8_steps(ks, LK, 32 * kb, 16 * S::kt(wv, i));
+    lds_barrier();
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) {
+        const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
+        wh[j][kb] = ld8(Zt + o);
+        wl[j][kb] = ld8(Zl + o);
+      }
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      z[t] = mfma_k32(uo[t][1], Tf[0], zero);
+      z[t] = mfma_k32(uh[t][1], Tf[1], z[t]);
+      z[t] = mfma_k32(uh[t][1], Tf[0], z[t]);
+      z[t] = mfma_k32(uo[t][0], Tf[2], z[t]);
+      z[t] = mfma_k32(uh[t][0], Tf[3], z[t]);
+      z[t] = mfma_k32(uh[t][0], Tf[2], z[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < VT; ++t) settle(z[t]);
+    const float back = inv * om;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], acc[i][j]);
+          acc[i][j] = mfma_k32(xT[i][kb], wh[j][kb], acc[i][j]);
+        }
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) {
+        settle(acc[i][j]);
+        D[i][j] = gc * D[i][j] + back * acc[i][j];
+      }
+    const float bz = b1 * inv;
+    take(max(ch - 1, 0));
+    const size_t at = (size_t)unit * chunks + ch;
+    const bool step = ch * C + 16 * wv + d < a.T;
+    char *o = dv0 + ch * in.vstep + (uint32_t)(16 * wv + d) * in.vrow + 8 * g4;
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       // (a lane's four columns are half of the eight that the operand's lane d + 16 (column / 8) holds)
       const int c = (VB == 32 ? 0 : 16 * (part & 1)) + 16 * t + 4 * g4, v32 = VB == 32 ? part : part >> 1;
       *(u2_t *)(rows_z + at * C * a.V + ((size_t)(v32 * 4 + wv) * 64 + d + 16 * (c >> 3)) * 8 + (c & 7)) = pack4_h(z[t]);
-      if (step < a.T) {
-        const f4_t o = (b1 * inv) * z[t];
-        *(u2_t *)((unsigned short *)a.dv + vbase + (size_t)step * vrow + 16 * t + 4 * g4) =
-            u2_t{pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3])};
-      }
+      const f4_t dv = bz * z[t];
+      if (step) *(u2_t *)(o + 32 * t) = u2_t{pack2_bf16(dv[0], dv[1]), pack2_bf16(dv[2], dv[3])};
     }
-  }
-  if (a.dH0)
+    size_t f;
+    if (KT >= 4 || wv < KT)
 #pragma unroll
-    for (int p = 0; p < PW; ++p) {
-      const int t = wv + 4 * p, kt = t % KT, vt = t / KT;
-      if (t < NT)
+      for (int i = 0; i < KTW; ++i)
+        if (frag_at<VB>(part, KT, S::kt(wv, i), f)) *(h8_t *)(dstates + at * K * a.V + f) = hs[i];
+    if (threadIdx.x == 0) scales[at * (a.V / VB) + part] = s;
+  }
+  if (a.dH0 && S::on(wv))
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          a.dH0[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + part * VB + 16 * vt + d] = D[p][x];
-    }
+          a.dH0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] = D[i][j][x];
 }
 
 // ------------------------------------------------------------------ dq, dk, dg, dbeta of one chunk
@@ -963,18 +1157,25 @@ int columns(const DeltaArgs &a) { (void)a; return 32; }
 
 template <bool BWD>
 hipError_t prep(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
-  hipLaunchKernelGGL(delta_half_prep_kernel<BWD>, dim3((unsigned)(a.B * a.N) * (unsigned)l.chunks), dim3(256), 0, s, a,
-                     l.chunks, w.gates, w.mats);
+  const dim3 grid((unsigned)(a.B * a.N) * (unsigned)l.chunks);
+  if (a.K == 32) hipLaunchKernelGGL((delta_half_prep_kernel<32, BWD>), grid, dim3(256), 0, s, a, l.chunks, w.gates, w.mats);
+  else if (a.K == 64) hipLaunchKernelGGL((delta_half_prep_kernel<64, BWD>), grid, dim3(256), 0, s, a, l.chunks, w.gates, w.mats);
+  else hipLaunchKernelGGL((delta_half_prep_kernel<128, BWD>), grid, dim3(256), 0, s, a, l.chunks, w.gates, w.mats);
+  return hipGetLastError();
+}
+template <int K, int VB, bool Y, bool CKPT>
+hipError_t fwd_go(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
+  constexpr int lds = lds_fwd<K, VB>();
+  const hipError_t e = set_max_lds_once(delta_half_fwd_kernel<K, VB, Y, CKPT>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((delta_half_fwd_kernel<K, VB, Y, CKPT>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a,
+                     l.chunks, w.gates, w.mats, (half_t *)a.ckpt, a.ckpt ? (half_t *)(a.ckpt + l.states) : nullptr);
   return hipGetLastError();
 }
 template <int K, int VB>
 hipError_t fwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
-  constexpr int lds = lds_fwd<K, VB>();
-  const hipError_t e = set_max_lds_once(delta_half_fwd_kernel<K, VB>, lds);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((delta_half_fwd_kernel<K, VB>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a, l.chunks, w.gates, w.mats, (half_t *)a.ckpt,
-                     a.ckpt ? (half_t *)(a.ckpt + l.states) : nullptr);
-  return hipGetLastError();
+  if (!a.write_y) return fwd_go<K, VB, false, true>(a, l, w, s);
+  return a.ckpt ? fwd_go<K, VB, true, true>(a, l, w, s) : fwd_go<K, VB, true, false>(a, l, w, s);
 }
 template <int K, int VB>
 hipError_t bwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
