@@ -18,8 +18,8 @@ m2rnn_status check(const m2rnn_desc *d) {
   // (units, and units times parts or chunks, are workgroup numbers)
   const double units = (double)d->B * d->N;
   if (units * 16 > 1e9 || units * (d->T / 32 + 1) > 2e9) return M2RNN_ERR_SHAPE;
-  // (a chunk's rows are reached by 32-bit offsets)
-  if ((double)d->N * d->V > (1 << 24) || (double)d->Nqk * d->K > (1 << 24)) return M2RNN_ERR_SHAPE;
+  // (a chunk's rows are reached by 31-bit byte offsets)
+  if ((double)d->N * d->V >= (1 << 23) || (double)d->Nqk * d->K >= (1 << 23)) return M2RNN_ERR_SHAPE;
   if (d->chunk != 0) return M2RNN_ERR_CHUNK;
   return M2RNN_OK;
 }

@@ -85,7 +85,11 @@ __device__ __forceinline__ h8_t ld8_tr(const half_t *base, int ld, int r0, int c
 // ------------------------------------------------------------------ gates, T, P of one chunk
 // T and P of a chunk: [row tile 4][32 columns 2][hi, lo][lane][8].  BWD: of their transposes.
 constexpr size_t kMat = 4 * 2 * 2 * 64 * 8;  // halfs
-__device__ __forceinline__ size_t mat_at(int tile, int kb, int part) { return (size_t)(((tile * 2 + kb) * 2 + part) * 64) * 8; }
+__device__ __forceinline__ int mat_at(int tile, int kb, int part) { return (((tile * 2 + kb) * 2 + part) * 64) * 8; }
+// the bytes of a lane's part of it, or beyond the buffer (reads as zero) where the block is zero
+__device__ __forceinline__ uint32_t mat_bytes(int tile, int kb, int part, bool there) {
+  return there ? 2 * mat_at(tile, kb, part) + 16 * (threadIdx.x & 63) : 2 * (uint32_t)kMat;
+}
 
 __device__ __forceinline__ f4_t mma_f32(f4_t a, f4_t b, f4_t c) {
 #pragma unroll
@@ -279,17 +283,12 @@ struct Scan {
   static __device__ __forceinline__ bool on(int w) { return KT >= 4 || w / KT < VT; }
 };
 // Where the operand that holds 16 rows x 32 columns of V goes: [V / 32][tiles][lane][8]; with VB = 16 a
-// workgroup has one half of the lanes.
+// workgroup has one half of the lanes, and its two halves the same.
 template <int VB>
-__device__ __forceinline__ bool frag_at(int part, int tiles, int tile, size_t &o) {
+__device__ __forceinline__ size_t frag_at(int part, int tiles, int tile) {
   const int lane = threadIdx.x & 63;
-  if constexpr (VB == 32) {
-    o = ((size_t)(part * tiles + tile) * 64 + lane) * 8;
-    return true;
-  } else {
-    o = ((size_t)((part >> 1) * tiles + tile) * 64 + (lane & 31) + 32 * (part & 1)) * 8;
-    return lane < 32;
-  }
+  if constexpr (VB == 32) return ((size_t)(part * tiles + tile) * 64 + lane) * 8;
+  else return ((size_t)((part >> 1) * tiles + tile) * 64 + (lane & 31) + 32 * (part & 1)) * 8;
 }
 // that operand, from an LDS array [VB][ld]: its rows are the columns c0 .. c0 + 15 (STEPS: c0 a tile of steps)
 template <int VB, bool STEPS>
@@ -308,38 +307,79 @@ __device__ __forceinline__ void pin8(h8_t &x) {
   x = __builtin_bit_cast(h8_t, y);
 }
 
-// A chunk's rows of q, k, v, dy, T, P: wave-uniform base and 32-bit offsets of the lanes (rows behind the last one
-// are the last one)
-template <int K, int VB>
-struct Chunk {
-  using S = Scan<K, VB>;
-  const char *q, *k, *v, *mats;
-  const float *gates;
-  size_t qstep, vstep;  // bytes of a chunk
-  uint32_t qrow, vrow;  // bytes of a row
+// Nothing moves across: a load stays behind the last use of the registers that it fills
+__device__ __forceinline__ void hold() { __builtin_amdgcn_sched_barrier(0); }
+
+// A chunk's rows of a [T][row] tensor through a buffer that ends with the sequence: what lies behind the last step
+// reads as zero and is not written, without a branch, and a lane's offset is the same for all chunks.
+struct Rows {
+  char *base;
+  uint32_t row;  // bytes
   int T;
-  __device__ __forceinline__ Chunk(const DeltaArgs &a, const void *vv, int unit, int part, int chunks,
-                                   const float *gts, const half_t *mts) {
-    const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
-    const size_t qr = (size_t)a.Nqk * K * 2, vr = (size_t)a.N * a.V * 2;
-    q = (const char *)a.q + (size_t)b * a.T * qr + (size_t)nq * K * 2;
-    k = (const char *)a.k + (size_t)b * a.T * qr + (size_t)nq * K * 2;
-    v = (const char *)vv + (size_t)b * a.T * vr + ((size_t)n * a.V + part * VB) * 2;
-    mats = (const char *)(mts + (size_t)unit * chunks * 2 * kMat);
-    gates = gts + (size_t)unit * chunks * kGates;
-    qstep = C * qr;
-    vstep = C * vr;
-    qrow = (uint32_t)qr;
-    vrow = (uint32_t)vr;
-    T = a.T;
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(int ch) const {
+    return __builtin_amdgcn_make_buffer_rsrc(base + (size_t)ch * C * row, 0, min(C, T - ch * C) * row, 0x00027000);
   }
-  __device__ __forceinline__ uint32_t at(int ch, int row, uint32_t stride) const {
-    return (uint32_t)min(row, T - 1 - ch * C) * stride;
+};
+__device__ __forceinline__ u4_t buf_ld(__amdgpu_buffer_rsrc_t r, uint32_t o) {
+  return __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0);
+}
+__device__ __forceinline__ h8_t buf_h8(__amdgpu_buffer_rsrc_t r, uint32_t o) { return __builtin_bit_cast(h8_t, buf_ld(r, o)); }
+__device__ __forceinline__ void buf_st(__amdgpu_buffer_rsrc_t r, uint32_t o, u2_t x) {
+  __builtin_amdgcn_raw_buffer_store_b64(x, r, o, 0, 0);
+}
+struct Place {  // of a workgroup
+  Rows q, k, v, o;  // o: y or dv, laid out as v (v or dy)
+  char *mats;
+  const float *gates;
+  // T (part 0) and P (part 1) of a chunk
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t mat(int ch, int part) const {
+    return __builtin_amdgcn_make_buffer_rsrc(mats + ((size_t)ch * 2 + part) * (2 * kMat), 0, 2 * kMat, 0x00027000);
+  }
+  __device__ __forceinline__ Place(const DeltaArgs &a, const void *v_, void *o_, int unit, int col, int chunks,
+                                   const float *gates_, const half_t *mats_) {
+    const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
+    const uint32_t qr = (uint32_t)a.Nqk * a.K * 2, vr = (uint32_t)a.N * a.V * 2;
+    const size_t qo = (size_t)b * a.T * qr + (size_t)nq * a.K * 2, vo = (size_t)b * a.T * vr + ((size_t)n * a.V + col) * 2;
+    q = Rows{(char *)a.q + qo, qr, a.T};
+    k = Rows{(char *)a.k + qo, qr, a.T};
+    v = Rows{(char *)v_ + vo, vr, a.T};
+    o = Rows{(char *)o_ + vo, vr, a.T};
+    mats = (char *)(mats_ + (size_t)unit * chunks * 2 * kMat);
+    gates = gates_ + (size_t)unit * chunks * kGates;
+  }
+};
+// What the wave's steps need of the gates, one float a lane in one load, through LDS to the lanes that use it
+struct Gates {
+  float *at;  // 64 of the wave
+  static __device__ __forceinline__ uint32_t offset(int wv) {
+    const int lane = threadIdx.x & 63, i = lane & 15;
+    return 4 * (lane < 16 ? 16 * wv + i : lane < 32 ? C + 16 * wv + i : lane < 48 ? 4 * C + 16 * wv + i : i == 0 ? C - 1 : 2 * C);
+  }
+  __device__ __forceinline__ f4_t four(int which) const { return *(const f4_t *)(at + 16 * which + 4 * ((threadIdx.x & 63) >> 4)); }
+  __device__ __forceinline__ float one(int which) const { return at[16 * which + (threadIdx.x & 15)]; }
+  __device__ __forceinline__ float last() const { return at[48]; }    // e^G of the chunk's last step
+  __device__ __forceinline__ float first() const { return at[49]; }   // hi of its first
+};
+// A wave's 16 steps of VB columns, eight a lane as loaded, through LDS to four steps of one column per lane and
+// column tile, as in D[step][column]
+template <int VB>
+struct Turn {
+  static constexpr int LD = VB + 8, HALFS = 16 * LD;  // per wave
+  half_t *at;
+  __device__ __forceinline__ void put(u4_t x) const {
+    const int lane = threadIdx.x & 63, g = VB == 32 ? lane >> 4 : (lane >> 4) & 1;
+    *(u4_t *)(at + (lane & 15) * LD + 8 * g) = x;
+  }
+  __device__ __forceinline__ f4_t get(int t) const {
+    const int lane = threadIdx.x & 63, d = lane & 15, g = lane >> 4;
+    const u2_t x = __builtin_bit_cast(u2_t, lds_ld_tr((const lchar *)(at + (4 * g + (d >> 2)) * LD + 16 * t + 4 * (d & 3)), 0));
+    return f4_t{__builtin_bit_cast(float, x.x << 16), __builtin_bit_cast(float, x.x & 0xFFFF0000u),
+                __builtin_bit_cast(float, x.y << 16), __builtin_bit_cast(float, x.y & 0xFFFF0000u)};
   }
 };
 
 template <int K, int VB>
-constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC) * 2; }
+constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4; }
 
 // Y: y is wanted;  CKPT: the chunks' states and U are
 template <int K, int VB, bool Y, bool CKPT>
@@ -350,18 +390,21 @@ __global__ void __launch_bounds__(256, 2)
   constexpr int KB = S::KB, KT = S::KT, VT = S::VT, KTW = S::KTW, VTW = S::VTW, LK = S::LK;
   extern __shared__ __align__(16) char lds[];
   half_t *ks = (half_t *)lds, *Ht = ks + C * LK, *Hl = Ht + VB * LK, *Rt = Hl + VB * LK, *Rl = Rt + VB * LC;
-  half_t *Ut = Rl + VB * LC, *Wt = Ut + VB * LC, *Wl = Wt + VB * LC;
+  half_t *Ut = Rl + VB * LC, *Wt = Ut + VB * LC, *Wl = Wt + VB * LC, *turn = Wl + VB * LC;
   int unit, part;
   if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int d = lane & 15, g4 = lane >> 4;
-  // T and P are lower triangular: the first two waves have no steps above 31, and zeros there (a branch around
-  // their products would not make the other two waves faster)
+  const Turn<VB> tv{turn + wv * Turn<VB>::HALFS};
+  const Gates gs{(float *)(turn + 4 * Turn<VB>::HALFS) + 64 * wv};
+  // T and P are lower triangular: the first two waves have no steps above 31, and read zeros there without a memory
+  // access (a branch around their products would not make the other two waves faster)
   const bool two = wv >= 2;
-  const Chunk<K, VB> in(a, a.v, unit, part, chunks, gates, mats);
-  char *y0 = (char *)a.y + (in.v - (const char *)a.v);
+  const Place in(a, a.v, a.y, unit, part * VB, chunks, gates, mats);
   const f4_t zero = {0.f, 0.f, 0.f, 0.f};
   const size_t state0 = (size_t)unit * K * a.V + part * VB + d;  // element (0, d) of my columns
+  const uint32_t oq = (16 * wv + d) * in.q.row + 16 * g4, og = Gates::offset(wv);
+  const uint32_t ov = (16 * wv + d) * in.v.row + 16 * (VB == 32 ? g4 : g4 & 1), oy = (16 * wv + d) * in.v.row + 8 * g4;
 
   f4_t H[KTW][VTW];
 #pragma unroll
@@ -371,73 +414,44 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         H[i][j][x] = a.H0 ? a.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
-  u4_t nk[KB], nq[KB], nT[4], nP[2];
-  unsigned short nv[VT][4];
-  f4_t nge, ngl, nbe;
-  float ng1, ngc;
-  auto fetch = [&](int ch) {
-    const char *k = in.k + ch * in.qstep, *q = in.q + ch * in.qstep, *v = in.v + ch * in.vstep;
-    const char *m = in.mats + (size_t)ch * 4 * kMat;
-    const float *gt = in.gates + (size_t)ch * kGates;
-    const uint32_t r = in.at(ch, 16 * wv + d, in.qrow) + 16 * g4;
-    const int kb = two ? 1 : 0;  // (unconditional: the first two waves read their only block again)
+  // The next chunk's, in the order of their use: k, v and gates in its first product, T in its second, q and P last.
+  // Each load is issued behind the last use of its registers and so has most of a chunk to arrive.
+  u4_t nk[KB], nq[KB], nv;
+  h8_t Tf[4], Pf[2];  // [32 steps][hi, lo];  [32 steps]
+  float ng;
+  auto fetch1 = [&](int ch) {
+    const auto k = in.k.at(ch), v = in.v.at(ch);
 #pragma unroll
-    for (int i = 0; i < KB; ++i) nk[i] = *(const u4_t *)(k + (r + 64 * i));
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const uint32_t rv = in.at(ch, 16 * wv + 4 * g4 + x, in.vrow) + 2 * d;
-#pragma unroll
-      for (int t = 0; t < VT; ++t) nv[t][x] = *(const unsigned short *)(v + (rv + 32 * t));
-    }
-    nge = *(const f4_t *)(gt + 16 * wv + 4 * g4);
-    nbe = *(const f4_t *)(gt + 4 * C + 16 * wv + 4 * g4);
-    ngl = *(const f4_t *)(gt + C + 16 * wv + 4 * g4);
-    ng1 = gt[16 * wv + d];
-    ngc = gt[C - 1];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      nT[i] = *(const u4_t *)(m + 2 * mat_at(wv, 0, i) + 16 * lane);
-      nT[2 + i] = *(const u4_t *)(m + 2 * mat_at(wv, kb, i) + 16 * lane);
-    }
-    if (Y) {
-      nP[0] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, 0, 0) + 16 * lane);
-      nP[1] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, kb, 0) + 16 * lane);
-#pragma unroll
-      for (int i = 0; i < KB; ++i) nq[i] = *(const u4_t *)(q + (r + 64 * i));
-    }
+    for (int i = 0; i < KB; ++i) nk[i] = buf_ld(k, oq + 64 * i);
+    nv = buf_ld(v, ov);
+    ng = *(const float *)((const char *)(in.gates + (size_t)ch * kGates) + og);
   };
-  h8_t kf[KB], qf[KB], Tf[4], Pf[2];
+  auto fetch2 = [&](int ch) {
+    const auto m = in.mat(ch, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Tf[i] = buf_h8(m, mat_bytes(wv, i >> 1, i & 1, i < 2 || two));
+  };
+  auto fetch3 = [&](int ch) {
+    const auto m = in.mat(ch, 1), q = in.q.at(ch);
+#pragma unroll
+    for (int i = 0; i < KB; ++i) nq[i] = buf_ld(q, oq + 64 * i);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) Pf[i] = buf_h8(m, mat_bytes(wv, i, 0, i < 1 || two));
+  };
+  h8_t kf[KB];
   f4_t vf[VT], ge, gl, be;
   float g1, gc;
-  auto take = [&]() {
+  auto take1 = [&]() {
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
       kf[i] = bf16_to_h8(nk[i]);
       pin8(kf[i]);
-      if (Y) {
-        qf[i] = bf16_to_h8(nq[i]);
-        pin8(qf[i]);
-      }
     }
+    tv.put(nv);
+    gs.at[lane] = ng;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      pin(nT[i]);
-      Tf[i] = __builtin_bit_cast(h8_t, i < 2 || two ? nT[i] : u4_t{0u, 0u, 0u, 0u});
-    }
-    if (Y)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        pin(nP[i]);
-        Pf[i] = __builtin_bit_cast(h8_t, i < 1 || two ? nP[i] : u4_t{0u, 0u, 0u, 0u});
-      }
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) vf[t][x] = bf16_bits_to_f32(nv[t][x]);
-      pin(vf[t]);
-    }
-    ge = nge; gl = ngl; be = nbe; g1 = ng1; gc = ngc;
-    pin(ge); pin(gl); pin(be); pin(g1); pin(gc);
+    for (int t = 0; t < VT; ++t) vf[t] = tv.get(t);
+    ge = gs.four(0); gl = gs.four(1); be = gs.four(2); g1 = gs.one(0); gc = gs.last();
   };
   auto put_state = [&]() {
     if (S::on(wv))
@@ -453,11 +467,14 @@ __global__ void __launch_bounds__(256, 2)
   };
   put_state();
   if (chunks > 0) {
-    fetch(0);
-    take();
+    fetch1(0);
+    fetch2(0);
+    if (Y) fetch3(0);
+    take1();
   }
   const int w = place(wv);
   for (int ch = 0; ch < chunks; ++ch) {
+    const int next = min(ch + 1, chunks - 1);
     lds_barrier();  // the state is there, and k of the chunk before has been read
     // R = beta (v - e^G K H): D[step][column]
     h8_t hh[VT][KB], hl[VT][KB];
@@ -469,9 +486,9 @@ __global__ void __launch_bounds__(256, 2)
         hh[t][i] = ld8(Ht + o);
         hl[t][i] = ld8(Hl + o);
       }
-    fetch(min(ch + 1, chunks - 1));
 #pragma unroll
     for (int i = 0; i < KB; ++i) *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
+    fetch1(next);
     f4_t x[VT], xl[VT];
 #pragma unroll
     for (int t = 0; t < VT; ++t) x[t] = xl[t] = zero;
@@ -509,11 +526,6 @@ __global__ void __launch_bounds__(256, 2)
       for (int kb = 0; kb < 2; ++kb) kT[i][kb] = ld8_steps(ks, LK, 32 * kb, 16 * S::kt(wv, i));
 #pragma unroll
     for (int t = 0; t < VT; ++t) y[t] = u[t] = ul[t] = zero;
-    if (Y)
-#pragma unroll
-      for (int i = 0; i < KB; ++i)
-#pragma unroll
-        for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf[i], y[t]);
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       u[t] = mfma_k32(Tf[0], rh[t][0], u[t]);
@@ -523,6 +535,9 @@ __global__ void __launch_bounds__(256, 2)
       ul[t] = mfma_k32(Tf[3], rh[t][1], ul[t]);
       ul[t] = mfma_k32(Tf[2], rl[t][1], ul[t]);
     }
+    hold();
+    fetch2(next);
+    hold();
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       settle(u[t]);
@@ -544,12 +559,14 @@ __global__ void __launch_bounds__(256, 2)
         wh[j][kb] = ld8(Wt + o);
         wl[j][kb] = ld8(Wl + o);
       }
-    if (Y)
+    if (Y) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int i = 0; i < KB; ++i) {
+        const h8_t qf = bf16_to_h8(nq[i]);
 #pragma unroll
-        for (int t = 0; t < VT; ++t) uf[t][kb] = ld8(Ut + (16 * t + d) * LC + 32 * kb + 8 * g4);
-    if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
+        for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf, y[t]);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < KTW; ++i)
 #pragma unroll
@@ -570,28 +587,34 @@ __global__ void __launch_bounds__(256, 2)
     put_state();
     if (Y) {
 #pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int t = 0; t < VT; ++t) uf[t][kb] = ld8(Ut + (16 * t + d) * LC + 32 * kb + 8 * g4);
+#pragma unroll
       for (int t = 0; t < VT; ++t) {
         y[t] = mfma_k32(uf[t][0], Pf[0], g1 * y[t]);
         y[t] = mfma_k32(uf[t][1], Pf[1], y[t]);
       }
+      hold();
+      fetch3(next);
+      hold();
 #pragma unroll
       for (int t = 0; t < VT; ++t) settle(y[t]);
     }
-    take();
-    if (Y && ch * C + 16 * wv + d < a.T) {
-      char *o = y0 + ch * in.vstep + (uint32_t)(16 * wv + d) * in.vrow + 8 * g4;
+    if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
+    take1();
+    if (Y) {
+      const auto o = in.o.at(ch);
 #pragma unroll
       for (int t = 0; t < VT; ++t)
-        *(u2_t *)(o + 32 * t) = u2_t{pack2_bf16(y[t][0], y[t][1]), pack2_bf16(y[t][2], y[t][3])};
+        buf_st(o, oy + 32 * t, u2_t{pack2_bf16(y[t][0], y[t][1]), pack2_bf16(y[t][2], y[t][3])});
     }
     if (CKPT) {
       const size_t at = (size_t)unit * chunks + ch;
-      size_t o;
       if (KT >= 4 || wv < KT)
 #pragma unroll
-        for (int i = 0; i < KTW; ++i)
-          if (frag_at<VB>(part, KT, S::kt(wv, i), o)) *(h8_t *)(states + at * K * a.V + o) = hs[i];
-      if (frag_at<VB>(part, 4, wv, o)) *(h8_t *)(rows_u + at * C * a.V + o) = us;
+        for (int i = 0; i < KTW; ++i) *(h8_t *)(states + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
+      *(h8_t *)(rows_u + at * C * a.V + frag_at<VB>(part, 4, wv)) = us;
     }
   }
   if (a.HT && S::on(wv))
@@ -608,7 +631,7 @@ __global__ void __launch_bounds__(256, 2)
 // largest |dH| and |dy| of the workgroup's columns: with unit keys nothing below exceeds some hundreds then, and
 // the pairs' 2^-25 is small.
 template <int K, int VB>
-constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC) * 2 + 16; }
+constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 16; }
 
 template <int K, int VB>
 __global__ void __launch_bounds__(256, 2)
@@ -620,14 +643,18 @@ __global__ void __launch_bounds__(256, 2)
   half_t *ks = (half_t *)lds, *qs = ks + C * LK, *Ht = qs + C * LK, *Hl = Ht + VB * LK, *Yt = Hl + VB * LK;
   half_t *Wt = Yt + VB * LC, *Wl = Wt + VB * LC, *Ut = Wl + VB * LC, *Ul = Ut + VB * LC;
   half_t *Zt = Wt, *Zl = Wl;  // (W has been read when Z comes)
-  float *red = (float *)(Ul + VB * LC);
+  half_t *turn = Ul + VB * LC;
+  float *red = (float *)(turn + 4 * Turn<VB>::HALFS) + 4 * 64;
   int unit, part;
   if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int d = lane & 15, g4 = lane >> 4;
+  const Turn<VB> ty{turn + wv * Turn<VB>::HALFS};
+  const Gates gs{(float *)(turn + 4 * Turn<VB>::HALFS) + 64 * wv};
   const bool two = wv < 2;  // (transposed: the last two waves have no steps below 32)
-  const Chunk<K, VB> in(a, a.dy, unit, part, chunks, gates, mats);
-  char *dv0 = (char *)a.dv + (in.v - (const char *)a.dy);
+  const Place in(a, a.dy, a.dv, unit, part * VB, chunks, gates, mats);
+  const uint32_t oq = (16 * wv + d) * in.q.row + 16 * g4, og = Gates::offset(wv);
+  const uint32_t ov = (16 * wv + d) * in.v.row + 16 * (VB == 32 ? g4 : g4 & 1), oo = (16 * wv + d) * in.v.row + 8 * g4;
   const f4_t zero = {0.f, 0.f, 0.f, 0.f};
   const size_t state0 = (size_t)unit * K * a.V + part * VB + d;
 
@@ -639,51 +666,35 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         D[i][j][x] = a.dHT ? a.dHT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
-  u4_t nk[KB], nq[KB], nT[4], nP[4];
-  unsigned short ny[VT][4];
-  f4_t nge, ngl, nbe;
-  float nb1, ngc, nom;
-  auto fetch = [&](int ch) {
-    const char *k = in.k + ch * in.qstep, *q = in.q + ch * in.qstep, *y = in.v + ch * in.vstep;
-    const char *m = in.mats + (size_t)ch * 4 * kMat;
-    const float *gt = in.gates + (size_t)ch * kGates;
-    const uint32_t r = in.at(ch, 16 * wv + d, in.qrow) + 16 * g4;
-    const int kb = two ? 0 : 1;  // (unconditional: the last two waves read their only block again)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const uint32_t rv = in.at(ch, 16 * wv + 4 * g4 + x, in.vrow) + 2 * d;
-#pragma unroll
-      for (int t = 0; t < VT; ++t) ny[t][x] = *(const unsigned short *)(y + (rv + 32 * t));
-    }
+  u4_t nk[KB], nq[KB], ny;
+  h8_t Tf[4], Pf[4];  // [32 steps, the later ones first][hi, lo]
+  float ng;
+  auto fetch1 = [&](int ch) {
+    const auto k = in.k.at(ch), q = in.q.at(ch), y = in.v.at(ch);
+    ny = buf_ld(y, ov);
+    ng = *(const float *)((const char *)(in.gates + (size_t)ch * kGates) + og);
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
-      nk[i] = *(const u4_t *)(k + (r + 64 * i));
-      nq[i] = *(const u4_t *)(q + (r + 64 * i));
-    }
-    nge = *(const f4_t *)(gt + 16 * wv + 4 * g4);
-    ngl = *(const f4_t *)(gt + C + 16 * wv + 4 * g4);
-    nbe = *(const f4_t *)(gt + 4 * C + 16 * wv + 4 * g4);
-    nb1 = gt[4 * C + 16 * wv + d];
-    nom = gt[2 * C];
-    ngc = gt[C - 1];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      nT[i] = *(const u4_t *)(m + 2 * mat_at(wv, 1, i) + 16 * lane);
-      nT[2 + i] = *(const u4_t *)(m + 2 * mat_at(wv, kb, i) + 16 * lane);
-      nP[i] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, 1, i) + 16 * lane);
-      nP[2 + i] = *(const u4_t *)(m + 2 * kMat + 2 * mat_at(wv, kb, i) + 16 * lane);
+      nk[i] = buf_ld(k, oq + 64 * i);
+      nq[i] = buf_ld(q, oq + 64 * i);
     }
   };
-  h8_t kf[KB], qf[KB], Tf[4], Pf[4];
+  auto fetch2 = [&](int ch) {
+    const auto m = in.mat(ch, 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Pf[i] = buf_h8(m, mat_bytes(wv, 1 - (i >> 1), i & 1, i < 2 || two));
+  };
+  auto fetch3 = [&](int ch) {
+    const auto m = in.mat(ch, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Tf[i] = buf_h8(m, mat_bytes(wv, 1 - (i >> 1), i & 1, i < 2 || two));
+  };
+  h8_t kf[KB], qf[KB];
   f4_t yf[VT], ge, gl, be;
   float b1, gc, om;
-  auto take = [&](int ch) {
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) yf[t][x] = ch * C + 16 * wv + 4 * g4 + x < a.T ? bf16_bits_to_f32(ny[t][x]) : 0.f;
-      pin(yf[t]);
-    }
+  auto take1 = [&]() {
+    ty.put(ny);
+    gs.at[lane] = ng;
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
       kf[i] = bf16_to_h8(nk[i]);
@@ -692,21 +703,20 @@ __global__ void __launch_bounds__(256, 2)
       pin8(qf[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      pin(nT[i]);
-      pin(nP[i]);
-      Tf[i] = __builtin_bit_cast(h8_t, i < 2 || two ? nT[i] : u4_t{0u, 0u, 0u, 0u});
-      Pf[i] = __builtin_bit_cast(h8_t, i < 2 || two ? nP[i] : u4_t{0u, 0u, 0u, 0u});
-    }
-    ge = nge; gl = ngl; be = nbe; b1 = nb1; om = gate_unit(nom); gc = om * ngc;
-    pin(ge); pin(gl); pin(be); pin(b1); pin(gc); pin(om);
+    for (int t = 0; t < VT; ++t) yf[t] = ty.get(t);
+    ge = gs.four(0); gl = gs.four(1); be = gs.four(2); b1 = gs.one(2);
+    om = gate_unit(gs.first());
+    gc = om * gs.last();
   };
   if (chunks > 0) {
-    fetch(chunks - 1);
-    take(chunks - 1);
+    fetch1(chunks - 1);
+    fetch2(chunks - 1);
+    fetch3(chunks - 1);
+    take1();
   }
   const int w = place(wv);
   for (int ch = chunks - 1; ch >= 0; --ch) {
+    const int next = max(ch - 1, 0);
     float top = 0.f;
 #pragma unroll
     for (int t = 0; t < VT; ++t)
@@ -764,7 +774,7 @@ __global__ void __launch_bounds__(256, 2)
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int t = 0; t < VT; ++t) yy[t][kb] = ld8(Yt + (16 * t + d) * LC + 32 * kb + 8 * g4);
-    fetch(max(ch - 1, 0));
+    fetch1(next);
     f4_t u[VT], ul[VT], py[VT];
 #pragma unroll
     for (int t = 0; t < VT; ++t) u[t] = ul[t] = py[t] = zero;
@@ -782,6 +792,9 @@ __global__ void __launch_bounds__(256, 2)
       py[t] = mfma_k32(Pf[2], yy[t][0], py[t]);
       py[t] = mfma_k32(Pf[3], yy[t][0], py[t]);
     }
+    hold();
+    fetch2(next);
+    hold();
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       settle(u[t]);
@@ -870,6 +883,9 @@ __global__ void __launch_bounds__(256, 2)
       z[t] = mfma_k32(uh[t][0], Tf[3], z[t]);
       z[t] = mfma_k32(uh[t][0], Tf[2], z[t]);
     }
+    hold();
+    fetch3(next);
+    hold();
 #pragma unroll
     for (int t = 0; t < VT; ++t) settle(z[t]);
     const float back = inv * om;
@@ -890,23 +906,20 @@ __global__ void __launch_bounds__(256, 2)
         D[i][j] = gc * D[i][j] + back * acc[i][j];
       }
     const float bz = b1 * inv;
-    take(max(ch - 1, 0));
+    take1();
     const size_t at = (size_t)unit * chunks + ch;
-    const bool step = ch * C + 16 * wv + d < a.T;
-    char *o = dv0 + ch * in.vstep + (uint32_t)(16 * wv + d) * in.vrow + 8 * g4;
+    const auto o = in.o.at(ch);
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       // (a lane's four columns are half of the eight that the operand's lane d + 16 (column / 8) holds)
       const int c = (VB == 32 ? 0 : 16 * (part & 1)) + 16 * t + 4 * g4, v32 = VB == 32 ? part : part >> 1;
       *(u2_t *)(rows_z + at * C * a.V + ((size_t)(v32 * 4 + wv) * 64 + d + 16 * (c >> 3)) * 8 + (c & 7)) = pack4_h(z[t]);
       const f4_t dv = bz * z[t];
-      if (step) *(u2_t *)(o + 32 * t) = u2_t{pack2_bf16(dv[0], dv[1]), pack2_bf16(dv[2], dv[3])};
+      buf_st(o, oo + 32 * t, u2_t{pack2_bf16(dv[0], dv[1]), pack2_bf16(dv[2], dv[3])});
     }
-    size_t f;
     if (KT >= 4 || wv < KT)
 #pragma unroll
-      for (int i = 0; i < KTW; ++i)
-        if (frag_at<VB>(part, KT, S::kt(wv, i), f)) *(h8_t *)(dstates + at * K * a.V + f) = hs[i];
+      for (int i = 0; i < KTW; ++i) *(h8_t *)(dstates + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
     if (threadIdx.x == 0) scales[at * (a.V / VB) + part] = s;
   }
   if (a.dH0 && S::on(wv))
