@@ -1166,7 +1166,7 @@ Ws carve(const DeltaLayout &l, char *p) {
 }
 
 // Columns of V per workgroup of the kernels that run in order
-int columns(const DeltaArgs &a) { (void)a; return 32; }
+int columns(const DeltaArgs &a) { return a.B * a.N * (a.V / 32) <= 128 ? 16 : 32; }
 
 template <bool BWD>
 hipError_t prep(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
