@@ -141,7 +141,8 @@ def _call():
                                % (built_for, torch.__version__, again))
         address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         module.init(address(L.m2rnn_fwd_opt), address(L.m2rnn_bwd_opt))
-        module.init_delta(address(L.m2rnn_delta_fwd), address(L.m2rnn_delta_bwd))
+        module.init_layer(address(L.m2rnn_delta_fwd), address(L.m2rnn_delta_bwd), address(L.m2rnn_group_norm_fwd),
+                          address(L.m2rnn_conv_silu_window_fwd))
         _call_module = module
     return _call_module
 
@@ -302,10 +303,8 @@ def m2rnn_gated_rmsnorm_bwd(y, a, w, eps, s, dout, dy, da, dw, workspace, stream
 
 def m2rnn_conv_silu_window_fwd(x, w, bias, win, out, win_out, stream=None, check=True):
     """m2rnn_conv_silu_fwd that starts from the steps in win [B,3,C] (None: zeros) and hands its last three
-    on in win_out (None: not wanted; may be win)."""
-    B, T, C = x.shape
-    rc = lib().m2rnn_conv_silu_window_fwd(B, T, C, _io_code(x), _ptr(x), _ptr(w), _ptr(bias), _ptr(win),
-                                          _ptr(out), _ptr(win_out), stream or 0)
+    on in win_out (None: not wanted; may be win).  Tensors are checked (ValueError)."""
+    rc = _call().window_fwd(x, w, bias, win, out, win_out, stream or 0)
     return _check(rc, "m2rnn_conv_silu_window_fwd", check)
 
 
@@ -315,14 +314,15 @@ def m2rnn_group_norm_workspace_bytes(B, T, D):
 
 def m2rnn_group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream=None, check=True):
     """out = n, SiLU(n) (M2RNN_NORM_SILU) or n SiLU(a): n is x [B,T,D], each token's `groups` groups of channels
-    normalised (M2RNN_NORM_CENTER: about their mean), times w [D] plus b [D] (None: 1, 0)."""
-    B, T, D = x.shape
-    rc = lib().m2rnn_group_norm_fwd(B, T, D, groups, _io_code(x), mode, _ptr(x), _ptr(a), _ptr(w), _ptr(b),
-                                    float(eps), _ptr(out), stream or 0)
+    normalised (M2RNN_NORM_CENTER: about their mean), times w [D] plus b [D] (None: 1, 0).  Tensors are
+    checked (ValueError)."""
+    rc = _call().group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream or 0)
     return _check(rc, "m2rnn_group_norm_fwd", check)
 
 
 def m2rnn_group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, stream=None, check=True):
+    """Gradients of m2rnn_group_norm_fwd: dx, da (with a), dw and db [D] fp32 (None: not wanted; without both no
+    workspace is needed)."""
     B, T, D = x.shape
     rc = lib().m2rnn_group_norm_bwd(B, T, D, groups, _io_code(x), mode, _ptr(x), _ptr(a), _ptr(w), _ptr(b),
                                     float(eps), _ptr(dout), _ptr(dx), _ptr(da), _ptr(dw), _ptr(db),
@@ -454,14 +454,13 @@ class Delta:
             self.dH0 = new(B, N, K, V, dtype=torch.float32)
         self.workspace = new(max(ws, 256), dtype=torch.uint8)
 
-    _stream = Scan._stream
-
     def fwd(self, q, k, v, g, beta, H0=None):
         """q, k [B,T,Nqk,K], v [B,T,N,V]; g [B,T,N] fp32 the log of the gate, beta [B,T,N] fp32.  H0 may be the HT of
-        the call before (a decode loop): the state is then carried in place."""
-        ws = self.workspace
+        the call before (a decode loop): the state is then carried in place.  A tensor of another size, type, GPU or
+        memory order is a ValueError."""
+        ws, dev = self.workspace, self.torch._C._cuda_getDevice()
         rc = self._native.delta_fwd(ctypes.addressof(self.desc), q, k, v, g, beta, H0, self.y, self.HT, self.ckpt, ws,
-                                    self._stream(), _nbytes(ws))
+                                    self.torch._C._cuda_getCurrentRawStream(dev), _nbytes(ws), dev)
         if rc != 0:
             raise M2RNNError(rc, "m2rnn_delta_fwd")
         return self.y, self.HT
@@ -469,9 +468,9 @@ class Delta:
     def bwd(self, q, k, v, g, beta, H0, dy, dHT=None, use_ckpt=True):
         """dq, dk, dv, dg, dbeta (io dtype) and dH0 (fp32)."""
         out = (self.dq, self.dk, self.dv, self.dg, self.dbeta, self.dH0)
-        ws = self.workspace
+        ws, dev = self.workspace, self.torch._C._cuda_getDevice()
         rc = self._native.delta_bwd(ctypes.addressof(self.desc), q, k, v, g, beta, H0, self.ckpt if use_ckpt else None,
-                                    dy, dHT, *out, ws, self._stream(), _nbytes(ws))
+                                    dy, dHT, *out, ws, self.torch._C._cuda_getCurrentRawStream(dev), _nbytes(ws), dev)
         if rc != 0:
             raise M2RNNError(rc, "m2rnn_delta_bwd")
         return out

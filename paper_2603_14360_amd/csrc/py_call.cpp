@@ -1,4 +1,5 @@
-// Python module _call: the entry points of the C ABI that Scan and Delta call, called with torch tensors.
+// Python module _call: entry points of the C ABI called with torch tensors: those of Scan and Delta, and the
+// forwards of the block's group norm and windowed convolution, which serving calls for every token.
 //
 // A decode step is one kernel of some 4 us, and handing its sixteen arguments over through ctypes took
 // 2.5 us of host time (on a slower host 6), beside a launch of 3.5.  Here the addresses are taken from the
@@ -15,6 +16,8 @@ decltype(&m2rnn_fwd_opt) fwd_opt = nullptr;
 decltype(&m2rnn_bwd_opt) bwd_opt = nullptr;
 decltype(&m2rnn_delta_fwd) delta_fwd = nullptr;
 decltype(&m2rnn_delta_bwd) delta_bwd = nullptr;
+decltype(&m2rnn_group_norm_fwd) group_norm_fwd = nullptr;
+decltype(&m2rnn_conv_silu_window_fwd) window_fwd = nullptr;
 
 // None -> NULL, an int as it is, a tensor -> its address, anything else -> what its data_ptr() says (a
 // subclass of the tensor may have its own); false with a Python error set otherwise
@@ -121,49 +124,173 @@ PyObject *bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   return PyLong_FromLong(st);
 }
 
-PyObject *init_delta(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  void *p[2];
-  if (!arity(n, 2) || !addresses(args, p)) return nullptr;
-  if (!p[0] || !p[1]) {
+PyObject *init_layer(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  void *p[4];
+  if (!arity(n, 4) || !addresses(args, p)) return nullptr;
+  if (!p[0] || !p[1] || !p[2] || !p[3]) {
     PyErr_SetString(PyExc_ValueError, "an entry point is NULL");
     return nullptr;
   }
   delta_fwd = (decltype(delta_fwd))p[0];
   delta_bwd = (decltype(delta_bwd))p[1];
+  group_norm_fwd = (decltype(group_norm_fwd))p[2];
+  window_fwd = (decltype(window_fwd))p[3];
   Py_RETURN_NONE;
 }
 
-// delta_fwd(desc, q, k, v, g, beta, H0, y, HT, ckpt, workspace, stream, bytes) -> status
+// An operand as `address` takes it; of a tensor also what the kernels assume of it: its type, its number of
+// elements, dense, on the GPU `device` that the call's stream belongs to (device < 0: any).
+bool operand(PyObject *o, const char *name, at::ScalarType type, int64_t count, long device, void *&p) {
+  if (!THPVariable_Check(o)) return address(o, p);
+  try {
+    const at::Tensor &t = THPVariable_Unpack(o);
+    const char *bad = !t.is_cuda() ? "is not on the GPU"
+                      : device >= 0 && t.get_device() != device ? "is on another GPU than the current one"
+                      : t.scalar_type() != type ? "has another dtype than the call takes"
+                      : t.numel() != count ? "has another size than the call takes"
+                      : !t.is_contiguous() ? "is not contiguous"
+                                           : nullptr;
+    if (bad) {
+      PyErr_Format(PyExc_ValueError, "%s %s", name, bad);
+      return false;
+    }
+    p = t.data_ptr();
+  } catch (const std::exception &e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return false;
+  }
+  return true;
+}
+at::ScalarType io_type(int32_t io) { return io == M2RNN_BF16 ? at::kBFloat16 : at::kFloat; }
+
+struct DeltaSizes {
+  int64_t qk, v, gates, state;
+  explicit DeltaSizes(const m2rnn_desc *d) {
+    const int64_t bt = (int64_t)d->B * d->T;
+    qk = bt * d->Nqk * d->K;
+    v = bt * d->N * d->V;
+    gates = bt * d->N;
+    state = (int64_t)d->B * d->N * d->K * d->V;
+  }
+};
+
+// delta_fwd(desc, q, k, v, g, beta, H0, y, HT, ckpt, workspace, stream, bytes, device) -> status
 PyObject *call_delta_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  void *p[12];
-  if (!ready((const void *)delta_fwd) || !arity(n, 13) || !addresses(args, p)) return nullptr;
+  if (!ready((const void *)delta_fwd) || !arity(n, 14)) return nullptr;
+  void *d, *q, *k, *v, *g, *beta, *H0, *y, *HT, *rest[3];
   const size_t bytes = PyLong_AsSize_t(args[12]);
-  if (bytes == (size_t)-1 && PyErr_Occurred()) return nullptr;
+  const long dev = PyLong_AsLong(args[13]);
+  if (PyErr_Occurred() || !address(args[0], d)) return nullptr;
+  const m2rnn_desc *desc = (const m2rnn_desc *)d;
+  const DeltaSizes z(desc);
+  const at::ScalarType io = io_type(desc->io), f = at::kFloat;
+  if (!operand(args[1], "q", io, z.qk, dev, q) || !operand(args[2], "k", io, z.qk, dev, k) ||
+      !operand(args[3], "v", io, z.v, dev, v) || !operand(args[4], "g", f, z.gates, dev, g) ||
+      !operand(args[5], "beta", f, z.gates, dev, beta) || !operand(args[6], "H0", f, z.state, dev, H0) ||
+      !operand(args[7], "y", io, z.v, dev, y) || !operand(args[8], "HT", f, z.state, dev, HT) ||
+      !addresses(args + 9, rest))
+    return nullptr;
   m2rnn_status st;
   Py_BEGIN_ALLOW_THREADS
-  st = delta_fwd((const m2rnn_desc *)p[0], p[1], p[2], p[3], (const float *)p[4], (const float *)p[5],
-                 (const float *)p[6], p[7], (float *)p[8], p[9], p[10], bytes, p[11]);
+  st = delta_fwd(desc, q, k, v, (const float *)g, (const float *)beta, (const float *)H0, y, (float *)HT, rest[0],
+                 rest[1], bytes, rest[2]);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
 
-// delta_bwd(desc, q, k, v, g, beta, H0, ckpt, dy, dHT, dq, dk, dv, dg, dbeta, dH0, workspace, stream, bytes) -> status
+// delta_bwd(desc, q, k, v, g, beta, H0, ckpt, dy, dHT, dq, dk, dv, dg, dbeta, dH0, workspace, stream, bytes, device)
+// -> status
 PyObject *call_delta_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  void *p[18];
-  if (!ready((const void *)delta_bwd) || !arity(n, 19) || !addresses(args, p)) return nullptr;
+  if (!ready((const void *)delta_bwd) || !arity(n, 20)) return nullptr;
+  void *d, *q, *k, *v, *g, *beta, *H0, *ckpt, *dy, *dHT, *out[8];
   const size_t bytes = PyLong_AsSize_t(args[18]);
-  if (bytes == (size_t)-1 && PyErr_Occurred()) return nullptr;
+  const long dev = PyLong_AsLong(args[19]);
+  if (PyErr_Occurred() || !address(args[0], d)) return nullptr;
+  const m2rnn_desc *desc = (const m2rnn_desc *)d;
+  const DeltaSizes z(desc);
+  const at::ScalarType io = io_type(desc->io), f = at::kFloat;
+  if (!operand(args[1], "q", io, z.qk, dev, q) || !operand(args[2], "k", io, z.qk, dev, k) ||
+      !operand(args[3], "v", io, z.v, dev, v) || !operand(args[4], "g", f, z.gates, dev, g) ||
+      !operand(args[5], "beta", f, z.gates, dev, beta) || !operand(args[6], "H0", f, z.state, dev, H0) ||
+      !address(args[7], ckpt) || !operand(args[8], "dy", io, z.v, dev, dy) ||
+      !operand(args[9], "dHT", f, z.state, dev, dHT) || !addresses(args + 10, out))
+    return nullptr;
   m2rnn_status st;
   Py_BEGIN_ALLOW_THREADS
-  st = delta_bwd((const m2rnn_desc *)p[0], p[1], p[2], p[3], (const float *)p[4], (const float *)p[5],
-                 (const float *)p[6], p[7], p[8], (const float *)p[9], p[10], p[11], p[12], p[13], p[14], (float *)p[15],
-                 p[16], bytes, p[17]);
+  st = delta_bwd(desc, q, k, v, (const float *)g, (const float *)beta, (const float *)H0, ckpt, dy, (const float *)dHT,
+                 out[0], out[1], out[2], out[3], out[4], (float *)out[5], out[6], bytes, out[7]);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// The sizes and the type of x [B,T,D]; false with a Python error set
+bool shape_of(PyObject *o, int32_t (&size)[3], int32_t &io, long &device) {
+  if (!THPVariable_Check(o)) {
+    PyErr_SetString(PyExc_TypeError, "x: expected a tensor");
+    return false;
+  }
+  const at::Tensor &t = THPVariable_Unpack(o);
+  if (t.dim() != 3 || (t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat)) {
+    PyErr_SetString(PyExc_ValueError, "x: expected three dimensions, float32 or bfloat16");
+    return false;
+  }
+  for (int i = 0; i < 3; ++i) {
+    if (t.size(i) > INT32_MAX) {
+      PyErr_SetString(PyExc_ValueError, "x: a dimension is too large");
+      return false;
+    }
+    size[i] = (int32_t)t.size(i);
+  }
+  io = t.scalar_type() == at::kBFloat16 ? M2RNN_BF16 : M2RNN_F32;
+  device = t.is_cuda() ? t.get_device() : -1;
+  return true;
+}
+
+// group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream) -> status
+PyObject *call_group_norm_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  int32_t s[3], io;
+  long dev;
+  if (!ready((const void *)group_norm_fwd) || !arity(n, 9) || !shape_of(args[0], s, io, dev)) return nullptr;
+  const long groups = PyLong_AsLong(args[4]), mode = PyLong_AsLong(args[6]);
+  const double eps = PyFloat_AsDouble(args[5]);
+  void *x, *a, *w, *b, *out, *stream;
+  const int64_t all = (int64_t)s[0] * s[1] * s[2];
+  const at::ScalarType t = io_type(io);
+  if (PyErr_Occurred() || !operand(args[0], "x", t, all, dev, x) || !operand(args[1], "a", t, all, dev, a) ||
+      !operand(args[2], "w", t, s[2], dev, w) || !operand(args[3], "b", t, s[2], dev, b) ||
+      !operand(args[7], "out", t, all, dev, out) || !address(args[8], stream))
+    return nullptr;
+  m2rnn_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = group_norm_fwd(s[0], s[1], s[2], (int32_t)groups, io, (int32_t)mode, x, a, w, b, (float)eps, out, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// window_fwd(x, w, bias, win, out, win_out, stream) -> status
+PyObject *call_window_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  int32_t s[3], io;
+  long dev;
+  if (!ready((const void *)window_fwd) || !arity(n, 7) || !shape_of(args[0], s, io, dev)) return nullptr;
+  void *x, *w, *bias, *win, *out, *win_out, *stream;
+  const int64_t all = (int64_t)s[0] * s[1] * s[2], rows = (int64_t)s[0] * 3 * s[2];
+  const at::ScalarType t = io_type(io);
+  if (!operand(args[0], "x", t, all, dev, x) || !operand(args[1], "w", t, 4 * (int64_t)s[2], dev, w) ||
+      !operand(args[2], "bias", t, s[2], dev, bias) || !operand(args[3], "win", t, rows, dev, win) ||
+      !operand(args[4], "out", t, all, dev, out) || !operand(args[5], "win_out", t, rows, dev, win_out) ||
+      !address(args[6], stream))
+    return nullptr;
+  m2rnn_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = window_fwd(s[0], s[1], s[2], io, x, w, bias, win, out, win_out, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
 
 PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)(void))init, METH_FASTCALL, nullptr},
-                         {"init_delta", (PyCFunction)(void (*)(void))init_delta, METH_FASTCALL, nullptr},
+                         {"init_layer", (PyCFunction)(void (*)(void))init_layer, METH_FASTCALL, nullptr},
+                         {"group_norm_fwd", (PyCFunction)(void (*)(void))call_group_norm_fwd, METH_FASTCALL, nullptr},
+                         {"window_fwd", (PyCFunction)(void (*)(void))call_window_fwd, METH_FASTCALL, nullptr},
                          {"delta_fwd", (PyCFunction)(void (*)(void))call_delta_fwd, METH_FASTCALL, nullptr},
                          {"delta_bwd", (PyCFunction)(void (*)(void))call_delta_bwd, METH_FASTCALL, nullptr},
                          {"fwd", (PyCFunction)(void (*)(void))fwd, METH_FASTCALL, nullptr},

@@ -127,3 +127,30 @@ def test_window_refusals():
     for n in ("x", "w", "bias", "win", "out", "win_out"):
         assert f(**{n: odd}) == 4
     assert f(B=0) == 0
+
+
+def cpu(*shape, dtype="float32"):
+    import torch
+    return torch.zeros(shape, dtype=getattr(torch, dtype))
+
+
+def test_tensors_that_are_not_on_the_gpu_are_refused():
+    """... before anything is launched; an address on the host would be read by the GPU."""
+    x, w = cpu(2, 3, 16), cpu(16)
+    with pytest.raises(ValueError, match="x is not on the GPU"):
+        mb.m2rnn_group_norm_fwd(x, None, w, None, 2, 1e-5, 0, cpu(2, 3, 16))
+    with pytest.raises(ValueError, match="x is not on the GPU"):
+        mb.m2rnn_conv_silu_window_fwd(x, cpu(16, 4), None, None, cpu(2, 3, 16), None)
+    for bad in (cpu(2, 16), cpu(2, 3, 16, dtype="float16"), cpu(2, 3, 16, dtype="float64")):
+        with pytest.raises(ValueError, match="x: expected"):
+            mb.m2rnn_group_norm_fwd(bad, None, w, None, 2, 1e-5, 0, cpu(2, 3, 16))
+    with pytest.raises(TypeError):
+        mb.m2rnn_group_norm_fwd(A, None, w, None, 2, 1e-5, 0, cpu(2, 3, 16))
+    d = desc()
+    args = [ctypes.addressof(d)] + [cpu(2, 70, 4, 32, dtype="bfloat16")] * 3 + [cpu(2, 70, 4)] * 2
+    with pytest.raises(ValueError, match="q is not on the GPU"):
+        mb._call().delta_fwd(*args, None, A, A, None, A, 0, 1 << 40, -1)
+    with pytest.raises(ValueError, match="q is not on the GPU"):
+        mb._call().delta_bwd(*args, None, A, A, None, A, A, A, A, A, A, A, 0, 1 << 40, -1)
+    with pytest.raises(TypeError):
+        mb._call().delta_fwd(*args)

@@ -284,3 +284,35 @@ def test_offsets_beyond_32_bits():
     wy, wH, _ = dr.rule_fwd(*(s[n] for n in ("q", "k", "v", "g", "beta")))
     check({"y": y[-1:], "HT": HT[-1:]}, {"y": wy, "HT": wH}, "large")
     assert not y[:-1].any() and not HT[:-1].any()
+
+
+def test_tensors_that_do_not_fit_are_refused():
+    """Another size, type or memory order: an exception, and nothing is launched."""
+    import torch
+    s = dr.rule_inputs(22, 2, 10, 4, 32, 64, Nqk=2, io="bf16")
+    d = device(s, "bf16")
+    p = mb.Delta(2, 10, 4, 32, 64, "bf16", Nqk=2)
+    names = ("q", "k", "v", "g", "beta", "H0")
+    good = [d[n] for n in names]
+    p.y.fill_(7)
+    for i, n in enumerate(names):
+        x = good[i]
+        for bad, why in ((x[:1], "size"), (x.double(), "dtype"), (x.cpu(), "not on the GPU"),
+                         (x.transpose(0, 1).contiguous().transpose(0, 1), "contiguous")):
+            args = good[:i] + [bad] + good[i + 1:]
+            with pytest.raises(ValueError, match="%s .*%s" % (n, why)):
+                p.fwd(*args)
+            with pytest.raises(ValueError, match="%s .*%s" % (n, why)):
+                p.bwd(*args, d["dy"], d["dHT"])
+    with pytest.raises(ValueError, match="dy"):
+        p.bwd(*good, d["dy"].float(), None)
+    with pytest.raises(mb.M2RNNError):
+        p.fwd(None, *good[1:])
+    torch.cuda.synchronize()
+    assert (p.y == 7).all()
+    x = torch.zeros(2, 3, 16, device="cuda")
+    for kw in (dict(w=torch.zeros(8, device="cuda")), dict(out=torch.zeros(2, 3, 16, device="cuda").bfloat16()),
+               dict(a=x[:, :2]), dict(b=torch.zeros(16))):
+        a = dict(dict(x=x, a=None, w=None, b=None, groups=2, eps=1e-5, mode=0, out=x.clone()), **kw)
+        with pytest.raises(ValueError):
+            mb.m2rnn_group_norm_fwd(**a)
