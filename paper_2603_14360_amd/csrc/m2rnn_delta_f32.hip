@@ -51,9 +51,10 @@ struct Ws {  // device pointers into the workspace
 
 // ------------------------------------------------------------------ gates, T, P of one chunk
 template <typename IO>
-__global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a, int chunks, float *__restrict__ gates,
+__global__ void __launch_bounds__(256, 2) delta_prep_kernel(DeltaArgs a, int chunks, float *__restrict__ gates,
                                                          float *__restrict__ mats) {
-  __shared__ float A[C][C + 1], hi[C], lo[C], be[C];
+  __shared__ __align__(16) float A[C][C + 4];
+  __shared__ float hi[C], lo[C], be[C];
   const int unit = blockIdx.x / chunks, ch = blockIdx.x - unit * chunks;
   const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
   const int t0 = ch * C, lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -103,12 +104,13 @@ __global__ void __launch_bounds__(256) delta_prep_kernel(DeltaArgs a, int chunks
     float x[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      float s = (int)threadIdx.x == i ? 1.f : 0.f;
+      float s[4] = {(int)threadIdx.x == i ? 1.f : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < i; ++j) s = fmaf(-A[i][j], x[j], s);
-      x[i] = s;
-      Tm[i * C + threadIdx.x] = s;
+      for (int j = 0; j < i; ++j) s[j & 3] = fmaf(-A[i][j], x[j], s[j & 3]);
+      x[i] = (s[0] + s[1]) + (s[2] + s[3]);
     }
+#pragma unroll
+    for (int i = 0; i < C; ++i) Tm[i * C + threadIdx.x] = x[i];
   }
 }
 
@@ -124,6 +126,10 @@ struct Rows {
       const int e = threadIdx.x + 256 * i, t = e / (K / 4), c = e - t * (K / 4);
       x[i] = load4<IO>(p, base + (size_t)(t0 + t) * row + 4 * c, t < C && t0 + t < T);
     }
+  }
+  __device__ __forceinline__ void pin() {  // (they have arrived here)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) asm volatile("" : "+v"(x[i]));
   }
   // row-major [C][K + 4] and / or transposed [K][LC]
   __device__ __forceinline__ void store(float *rows, float *cols) const {
@@ -145,7 +151,7 @@ constexpr int lds_bwd(int K) { return (C * (K + 4) + 2 * K * LC + VB * (K + 4) +
 
 // ------------------------------------------------------------------ forward, chunks in order
 template <typename IO, int K>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
     delta_fwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const float *__restrict__ mats,
                      float *__restrict__ states, float *__restrict__ rows_u) {
   constexpr int KT = K / 16, PW = (KT + 3) / 4;  // row tiles of the state; of a wave: wave, wave + 4
@@ -169,20 +175,32 @@ __global__ void __launch_bounds__(256)
     for (int x = 0; x < 4; ++x)
       H[p][x] = a.H0 && kt < KT ? a.H0[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + vb * VB + l16] : 0.f;
   }
+  // The next chunk's inputs, in flight for a whole chunk and taken before this one's results are stored: the counter
+  // that a wait for loads looks at counts stores as well, in order.
+  const int tt = 16 * (wv & 1) + l16;
   Rows<IO, K> q, k;
-  f4_t tm, pm;
+  f4_t tm, pm, nv;
   float gv = 0.f;
   auto fetch = [&](int ch) {
     const int t0 = ch * C;
     const size_t at = (size_t)unit * chunks + ch;
     q.load(a.q, qbase, qrow, t0, a.T);
     k.load(a.k, qbase, qrow, t0, a.T);
+    nv = load4<IO>(a.v, vbase + (size_t)(t0 + tt) * vrow, t0 + tt < a.T);
     tm = *(const f4_t *)(mats + at * 2 * C * C + 4 * tid);
     pm = *(const f4_t *)(mats + at * 2 * C * C + C * C + 4 * tid);
     if (tid < 2 * C) gv = gates[at * 4 * C + tid];
     else if (tid < 3 * C) gv = t0 + tid - 2 * C < a.T ? a.beta[((size_t)b * a.T + t0 + tid - 2 * C) * a.N + n] : 0.f;
   };
-  if (chunks > 0) fetch(0);
+  auto arrived = [&]() {
+    q.pin();
+    k.pin();
+    asm volatile("" : "+v"(tm), "+v"(pm), "+v"(nv), "+v"(gv));
+  };
+  if (chunks > 0) {
+    fetch(0);
+    arrived();
+  }
   for (int ch = 0; ch < chunks; ++ch) {
     const int t0 = ch * C;
     q.store(qs, nullptr);
@@ -193,20 +211,13 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
     for (int p = 0; p < PW; ++p) {
       const int kt = wv + 4 * p;
-      if (kt < KT) {
-        *(f4_t *)&Ht[l16 * (K + 4) + 16 * kt + 4 * g4] = H[p];
-        if (states)
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            states[(((size_t)unit * chunks + ch) * K + 16 * kt + 4 * g4 + x) * a.V + vb * VB + l16] = H[p][x];
-      }
+      if (kt < KT) *(f4_t *)&Ht[l16 * (K + 4) + 16 * kt + 4 * g4] = H[p];
     }
     // v of my column of the 16 x 16 tile [V][steps]: wave 0 and 1 the chunk's first and second 16 steps
-    const int tt = 16 * (wv & 1) + l16;
     const bool tok = t0 + tt < a.T;
-    const f4_t v = load4<IO>(a.v, vbase + (size_t)(t0 + tt) * vrow, tok);
-    __syncthreads();
-    if (ch + 1 < chunks) fetch(ch + 1);
+    const f4_t v = nv;
+    lds_barrier();
+    fetch(min(ch + 1, chunks - 1));
     // waves 0, 1: (K H)^T;  waves 2, 3: (Q H)^T
     const f4_t zero = {0.f, 0.f, 0.f, 0.f};
     f4_t xh = mma_rows(Ht + l16 * (K + 4) + 4 * g4, (wv < 2 ? ks : qs) + tt * (K + 4) + 4 * g4, K, zero);
@@ -216,30 +227,42 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
       for (int x = 0; x < 4; ++x) Rt[(4 * g4 + x) * LC + tt] = bt * (v[x] - gm * xh[x]);
     }
-    __syncthreads();
+    lds_barrier();
+    f4_t u = zero;
     if (wv < 2) {
-      const f4_t u = mma_rows(Rt + l16 * LC + 4 * g4, Ts + tt * LC + 4 * g4, C, zero);
+      u = mma_rows(Rt + l16 * LC + 4 * g4, Ts + tt * LC + 4 * g4, C, zero);
       const float gt = gl[tt];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         Ut[(4 * g4 + x) * LC + tt] = u[x];
         Wt[(4 * g4 + x) * LC + tt] = gt * u[x];
       }
-      if (rows_u && tok) *(f4_t *)&rows_u[vbase + (size_t)(t0 + tt) * vrow] = u;
     }
-    __syncthreads();
-    if (wv >= 2 && a.write_y) {
-      xh = mma_rows(Ut + l16 * LC + 4 * g4, Ps + tt * LC + 4 * g4, C, gm * xh);
-      if (tok) store4<IO>(a.y, vbase + (size_t)(t0 + tt) * vrow, xh);
-    }
+    lds_barrier();
+    if (wv >= 2 && a.write_y) xh = mma_rows(Ut + l16 * LC + 4 * g4, Ps + tt * LC + 4 * g4, C, gm * xh);
     const float gc = ge[C - 1];
+    f4_t H0[PW];
+#pragma unroll
+    for (int p = 0; p < PW; ++p) H0[p] = H[p];
 #pragma unroll
     for (int p = 0; p < PW; ++p) {
       const int kt = wv + 4 * p;
       if (kt < KT)
         H[p] = mma_rows(kT + (16 * kt + l16) * LC + 4 * g4, Wt + l16 * LC + 4 * g4, C, gc * H[p]);
     }
-    __syncthreads();
+    arrived();
+    if (tok && wv >= 2 && a.write_y) store4<IO>(a.y, vbase + (size_t)(t0 + tt) * vrow, xh);
+    if (tok && wv < 2 && rows_u) *(f4_t *)&rows_u[vbase + (size_t)(t0 + tt) * vrow] = u;
+    if (states)
+#pragma unroll
+      for (int p = 0; p < PW; ++p) {
+        const int kt = wv + 4 * p;
+        if (kt < KT)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            states[(((size_t)unit * chunks + ch) * K + 16 * kt + 4 * g4 + x) * a.V + vb * VB + l16] = H0[p][x];
+      }
+    lds_barrier();
   }
   if (a.HT)
 #pragma unroll
@@ -254,7 +277,7 @@ __global__ void __launch_bounds__(256)
 
 // ------------------------------------------------------------------ backward, chunks in reverse order
 template <typename IO, int K>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
     delta_bwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const float *__restrict__ mats,
                      float *__restrict__ states, float *__restrict__ rows_z) {
   constexpr int KT = K / 16, PW = (KT + 3) / 4;
@@ -278,20 +301,32 @@ __global__ void __launch_bounds__(256)
     for (int x = 0; x < 4; ++x)
       D[p][x] = a.dHT && kt < KT ? a.dHT[((size_t)unit * K + 16 * kt + 4 * g4 + x) * a.V + vb * VB + l16] : 0.f;
   }
+  // The next chunk's inputs, in flight for a whole chunk and taken before this one's results are stored: the counter
+  // that a wait for loads looks at counts stores as well, in order.
+  const int tt = 16 * (wv & 1) + l16;
   Rows<IO, K> q, k;
-  f4_t tm, pm;
+  f4_t tm, pm, nv;
   float gv = 0.f;
   auto fetch = [&](int ch) {
     const int t0 = ch * C;
     const size_t at = (size_t)unit * chunks + ch;
     q.load(a.q, qbase, qrow, t0, a.T);
     k.load(a.k, qbase, qrow, t0, a.T);
+    nv = load4<IO>(a.dy, vbase + (size_t)(t0 + tt) * vrow, t0 + tt < a.T);
     tm = *(const f4_t *)(mats + at * 2 * C * C + 4 * tid);
     pm = *(const f4_t *)(mats + at * 2 * C * C + C * C + 4 * tid);
     if (tid < 2 * C) gv = gates[at * 4 * C + tid];
     else if (tid < 3 * C) gv = t0 + tid - 2 * C < a.T ? a.beta[((size_t)b * a.T + t0 + tid - 2 * C) * a.N + n] : 0.f;
   };
-  if (chunks > 0) fetch(chunks - 1);
+  auto arrived = [&]() {
+    q.pin();
+    k.pin();
+    asm volatile("" : "+v"(tm), "+v"(pm), "+v"(nv), "+v"(gv));
+  };
+  if (chunks > 0) {
+    fetch(chunks - 1);
+    arrived();
+  }
   for (int ch = chunks - 1; ch >= 0; --ch) {
     const int t0 = ch * C;
     q.store(nullptr, qT);
@@ -305,17 +340,11 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
     for (int p = 0; p < PW; ++p) {
       const int kt = wv + 4 * p;
-      if (kt < KT) {
-        *(f4_t *)&Ht[l16 * (K + 4) + 16 * kt + 4 * g4] = D[p];
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          states[(((size_t)unit * chunks + ch) * K + 16 * kt + 4 * g4 + x) * a.V + vb * VB + l16] = D[p][x];
-      }
+      if (kt < KT) *(f4_t *)&Ht[l16 * (K + 4) + 16 * kt + 4 * g4] = D[p];
     }
-    const int tt = 16 * (wv & 1) + l16;
     const bool tok = t0 + tt < a.T;
-    const f4_t dy = load4<IO>(a.dy, vbase + (size_t)(t0 + tt) * vrow, tok);
-    __syncthreads();
+    const f4_t dy = nv;
+    lds_barrier();
     const float gm = ge[tt], bt = be[tt];
     if (wv < 2)
 #pragma unroll
@@ -323,8 +352,8 @@ __global__ void __launch_bounds__(256)
         Yt[(4 * g4 + x) * LC + tt] = dy[x];
         Wt[(4 * g4 + x) * LC + tt] = gm * dy[x];
       }
-    __syncthreads();
-    if (ch > 0) fetch(ch - 1);
+    lds_barrier();
+    fetch(max(ch - 1, 0));
     const f4_t zero = {0.f, 0.f, 0.f, 0.f};
     if (wv < 2) {
       f4_t u = mma_rows(Ht + l16 * (K + 4) + 4 * g4, ks + tt * (K + 4) + 4 * g4, K, zero);
@@ -332,18 +361,18 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
       for (int x = 0; x < 4; ++x) Ut[(4 * g4 + x) * LC + tt] = u[x];
     }
-    __syncthreads();
+    lds_barrier();
+    f4_t z = zero;
     if (wv < 2) {
-      const f4_t z = mma_rows(Ut + l16 * LC + 4 * g4, Tt + tt * LC + 4 * g4, C, zero);
+      z = mma_rows(Ut + l16 * LC + 4 * g4, Tt + tt * LC + 4 * g4, C, zero);
 #pragma unroll
       for (int x = 0; x < 4; ++x) Zt[(4 * g4 + x) * LC + tt] = -bt * gm * z[x];
-      if (tok) {
-        *(f4_t *)&rows_z[vbase + (size_t)(t0 + tt) * vrow] = z;
-        store4<IO>(a.dv, vbase + (size_t)(t0 + tt) * vrow, bt * z);
-      }
     }
-    __syncthreads();
+    lds_barrier();
     const float gc = ge[C - 1];
+    f4_t D0[PW];
+#pragma unroll
+    for (int p = 0; p < PW; ++p) D0[p] = D[p];
 #pragma unroll
     for (int p = 0; p < PW; ++p) {
       const int kt = wv + 4 * p;
@@ -352,7 +381,20 @@ __global__ void __launch_bounds__(256)
         D[p] = mma_rows(kT + (16 * kt + l16) * LC + 4 * g4, Zt + l16 * LC + 4 * g4, C, D[p]);
       }
     }
-    __syncthreads();
+    arrived();
+    if (tok && wv < 2) {
+      *(f4_t *)&rows_z[vbase + (size_t)(t0 + tt) * vrow] = z;
+      store4<IO>(a.dv, vbase + (size_t)(t0 + tt) * vrow, bt * z);
+    }
+#pragma unroll
+    for (int p = 0; p < PW; ++p) {
+      const int kt = wv + 4 * p;
+      if (kt < KT)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          states[(((size_t)unit * chunks + ch) * K + 16 * kt + 4 * g4 + x) * a.V + vb * VB + l16] = D0[p][x];
+    }
+    lds_barrier();
   }
   if (a.dH0)
 #pragma unroll
@@ -369,7 +411,7 @@ __global__ void __launch_bounds__(256)
 // Waves own column tiles wave, wave + 4 of K for both 16-step halves, and tile `wave` of S1 and S2.
 // Operands over V come straight from memory, four neighbours a lane.
 template <typename IO, int K>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
     delta_grad_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const float *__restrict__ states,
                       const float *__restrict__ rows_u, const float *__restrict__ dstates,
                       const float *__restrict__ rows_z, float *__restrict__ dq_heads, float *__restrict__ dk_heads) {
