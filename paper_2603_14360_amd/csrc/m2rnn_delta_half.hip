@@ -933,9 +933,13 @@ __global__ void __launch_bounds__(256, 2)
 }
 
 // ------------------------------------------------------------------ dq, dk, dg, dbeta of one chunk
-// Wave w has the chunk's steps 16 w .. 16 w + 15 and all of K: D[row of K][step].
+// Wave w has the chunk's steps 16 w .. 16 w + 15 and all of K: D[row of K][step].  S1 and S2 go through LDS to
+// the operands that the last products take.  With V <= 64 the products with H and dH come after that, in a loop of
+// their own: with all loads of a short loop in flight the two are faster (8 x 4096 steps, 16 heads of 64 x 64: 185 us,
+// 4.4 TB/s, against 198 in one).  With more blocks of 32 columns the second reading of y, z and U costs more than that
+// gives (4 x 8192, 8 of 128 x 128: 294 us against 223 in one loop).
 template <int K>
-constexpr int lds_grad() { return (2 * C * (K + 8) + 3 * C * LC) * 2 + (6 * C + 4 * 4) * 4; }
+constexpr int lds_grad() { return (2 * C * (K + 8) + 2 * C * LC + C) * 2 + (6 * C + 4 * 4) * 4; }
 
 __device__ __forceinline__ float dot8(h8_t a, h8_t b, float c) {
 #pragma unroll
@@ -943,119 +947,133 @@ __device__ __forceinline__ float dot8(h8_t a, h8_t b, float c) {
     c = __builtin_amdgcn_fdot2(h2_t{a[i], a[i + 1]}, h2_t{b[i], b[i + 1]}, c, false);
   return c;
 }
+// eight bf16 values times s, as fp16
+__device__ __forceinline__ h8_t bf16_to_h8(u4_t w, float s) {
+  u4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = w[i];
+    r[i] = pack2_h(s * __builtin_bit_cast(float, x << 16), s * __builtin_bit_cast(float, x & 0xFFFF0000u));
+  }
+  return __builtin_bit_cast(h8_t, r);
+}
 
-template <int K>
-__global__ void __launch_bounds__(256, 2)
+template <int K, int V32>
+__global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
     delta_half_grad_kernel(DeltaArgs a, int chunks, int vbs, const float *__restrict__ gates,
                            const half_t *__restrict__ states, const half_t *__restrict__ rows_u,
                            const half_t *__restrict__ dstates, const half_t *__restrict__ rows_z,
                            const float *__restrict__ scales, float *__restrict__ dq_heads, float *__restrict__ dk_heads) {
   constexpr int KB = K / 32, KT = K / 16, LK = K + 8;
+  constexpr bool ONE = V32 > 2;
   extern __shared__ __align__(16) char lds[];
-  half_t *ks = (half_t *)lds, *qs = ks + C * LK, *S1 = qs + C * LK, *S2 = S1 + C * LC, *Sb = S2 + C * LC;
-  float *ge = (float *)(Sb + C * LC), *red = ge + 5 * C;  // e^G, e^{G_C - G}, hi, lo, beta;  [4][4] and dG [C]
+  half_t *ks = (half_t *)lds, *qs = ks + C * LK, *S1 = qs + C * LK, *S2 = S1 + C * LC, *bh = S2 + C * LC;
+  float *ge = (float *)(bh + C), *red = ge + 5 * C;  // e^G, e^{G_C - G}, hi, lo, beta;  [4][4] and dG [C]
   const int unit = blockIdx.x / chunks, ch = blockIdx.x - unit * chunks, t0 = ch * C;
   const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int d = lane & 15, g4 = lane >> 4;
+  const int d = lane & 15, g4 = lane >> 4, i = 16 * wv + d, own = t0 + i;
   const size_t at = (size_t)blockIdx.x;
-  const size_t qrow = (size_t)a.Nqk * K, qbase = (size_t)b * a.T * qrow + (size_t)nq * K;
-  const size_t vrow = (size_t)a.N * a.V, vbase = (size_t)b * a.T * vrow + (size_t)n * a.V + 8 * g4;
-  const unsigned short *q = (const unsigned short *)a.q, *k = (const unsigned short *)a.k;
-  const unsigned short *dy = (const unsigned short *)a.dy, *v = (const unsigned short *)a.v;
+  const Place in(a, a.dy, a.dv, unit, 0, chunks, gates, nullptr);
+  const Rows v_{(char *)a.v + (in.v.base - (char *)a.dy), in.v.row, a.T};
+  const auto rq = in.q.at(ch), rk = in.k.at(ch), ry = in.v.at(ch), rv = v_.at(ch);
+  const uint32_t oq = i * in.q.row + 16 * g4, ov = i * in.v.row + 16 * g4;
   const f4_t zero = {0.f, 0.f, 0.f, 0.f};
-  const int own = t0 + 16 * wv + d, clamped = min(own, a.T - 1);
+  // (everything that depends on nothing: in flight together)
+  u4_t qr[KB], kr[KB];
 #pragma unroll
-  for (int i = 0; i < KB; ++i) {
-    const size_t o = qbase + (size_t)clamped * qrow + 32 * i + 8 * g4;
-    *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = bf16_to_h8(*(const u4_t *)(k + o));
-    *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = bf16_to_h8(*(const u4_t *)(q + o));
+  for (int e = 0; e < KB; ++e) {
+    kr[e] = buf_ld(rk, oq + 64 * e);
+    qr[e] = buf_ld(rq, oq + 64 * e);
   }
-  for (int i = threadIdx.x; i < kGates; i += 256) ge[i] = gates[at * kGates + i];
+  const half_t *U = rows_u + at * C * a.V + lane * 8, *Z = rows_z + at * C * a.V + (size_t)wv * 512 + lane * 8;
+  const half_t *h0 = states + at * K * a.V + lane * 8, *h1 = dstates + at * K * a.V + lane * 8;
   // the chunk's common power of two: that of the block with the largest gradients
   const int blocks = a.V / vbs;
-  float sc = scales[at * blocks];
-  for (int i = 1; i < blocks; ++i) sc = fminf(sc, scales[at * blocks + i]);
+  const float *sb = scales + at * blocks;
+  float sc = sb[0];
+  for (int x = 1; x < blocks; ++x) sc = fminf(sc, sb[x]);
+  auto factor = [&](int vb) {  // brings a block of 32 columns of Z or dH to it
+    const float s = vbs == 32 ? sb[vb] : g4 < 2 ? sb[2 * vb] : sb[2 * vb + 1];
+    const half_t f = (half_t)(sc * __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, s)));  // sc / s
+    return h8_t{f, f, f, f, f, f, f, f};
+  };
 
-  f4_t dq[KT], as[KT], kept[KT], s1[4], s2[4];
 #pragma unroll
-  for (int i = 0; i < KT; ++i) dq[i] = as[i] = kept[i] = zero;
+  for (int e = 0; e < KB; ++e) {
+    *(h8_t *)&ks[i * LK + 32 * e + 8 * g4] = bf16_to_h8(kr[e]);
+    *(h8_t *)&qs[i * LK + 32 * e + 8 * g4] = bf16_to_h8(qr[e]);
+  }
+  for (int x = threadIdx.x; x < kGates; x += 256) {
+    const float g = gates[at * kGates + x];
+    ge[x] = g;
+    if (x >= 4 * C) bh[x - 4 * C] = (half_t)g;
+  }
+
+  f4_t s1[4], s2[4], dq[KT], as[KT], kept[KT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) s1[i] = s2[i] = zero;
+  for (int j = 0; j < 4; ++j) s1[j] = s2[j] = zero;
+#pragma unroll
+  for (int x = 0; x < KT; ++x) dq[x] = as[x] = kept[x] = zero;
   float zv = 0.f, hd = 0.f;
-  for (int vb = 0; vb < a.V / 32; ++vb) {
-    const float f = sc / scales[at * blocks + (vbs == 32 ? vb : 2 * vb + (g4 >> 1))];
-    const half_t fh = (half_t)f;
-    const h8_t f8 = {fh, fh, fh, fh, fh, fh, fh, fh};
-    const half_t *U = rows_u + at * C * a.V + (size_t)vb * 4 * 512 + lane * 8;
-    const h8_t z = ld8(rows_z + at * C * a.V + (size_t)(vb * 4 + wv) * 512 + lane * 8) * f8;
-    const u4_t yr = *(const u4_t *)(dy + vbase + (size_t)clamped * vrow + 32 * vb);
-    const u4_t vr = *(const u4_t *)(v + vbase + (size_t)clamped * vrow + 32 * vb);
-    float yy[8], vv[8];
-    bf16x8_to_f32(yr, yy);
-    bf16x8_to_f32(vr, vv);
-    const float sy = own < a.T ? sc : 0.f;
-    const u4_t yp = {pack2_h(own < a.T ? sy * yy[0] : 0.f, own < a.T ? sy * yy[1] : 0.f),
-                     pack2_h(own < a.T ? sy * yy[2] : 0.f, own < a.T ? sy * yy[3] : 0.f),
-                     pack2_h(own < a.T ? sy * yy[4] : 0.f, own < a.T ? sy * yy[5] : 0.f),
-                     pack2_h(own < a.T ? sy * yy[6] : 0.f, own < a.T ? sy * yy[7] : 0.f)};
-    const h8_t y = __builtin_bit_cast(h8_t, yp);
+  auto with_states = [&](int vb, h8_t f8, h8_t y, h8_t z, h8_t u) {
+    const h8_t uf = u * f8;  // (for dH, whose power of two it is)
+    float hb = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) zv = fmaf((float)z[i], vv[i], zv);
-    h8_t u = {};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)  // D[j][i], j <= i
-      if (j <= wv) {
-        const h8_t uj = ld8(U + j * 512);
-        s1[j] = mfma_k32(uj, y, s1[j]);
-        s2[j] = mfma_k32(uj, z, s2[j]);
-        u = uj;  // (the last one is my own)
-      }
-    const half_t *h0 = states + at * K * a.V + (size_t)vb * KT * 512 + lane * 8;
-    const half_t *h1 = dstates + at * K * a.V + (size_t)vb * KT * 512 + lane * 8;
-#pragma unroll
-    for (int i = 0; i < KT; ++i) {
-      const h8_t x0 = ld8(h0 + i * 512), x1 = ld8(h1 + i * 512) * f8;
-      dq[i] = mfma_k32(x0, y, dq[i]);
-      as[i] = mfma_k32(x0, z, as[i]);
-      kept[i] = mfma_k32(x1, u, kept[i]);
-      if ((i & 3) == wv) hd = dot8(x0, x1, hd);
+    for (int x = 0; x < KT; ++x) {
+      const h8_t x0 = ld8(h0 + (vb * KT + x) * 512), x1 = ld8(h1 + (vb * KT + x) * 512);
+      dq[x] = mfma_k32(x0, y, dq[x]);
+      as[x] = mfma_k32(x0, z, as[x]);
+      kept[x] = mfma_k32(x1, uf, kept[x]);
+      if ((x & 3) == wv) hb = dot8(x0, x1, hb);
     }
-  }
+    hd = fmaf((float)f8[0], hb, hd);
+  };
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    settle(s1[i]);
-    settle(s2[i]);
-  }
+  for (int vb = 0; vb < (ONE ? 1 : V32); ++vb)
+#pragma unroll 1
+    for (int vo = vb; vo < (ONE ? V32 : vb + 1); ++vo) {
+      const h8_t f8 = factor(vo), z = ld8(Z + vo * 2048) * f8, y = bf16_to_h8(buf_ld(ry, ov + 64 * vo), sc);
+      float vv[8];
+      bf16x8_to_f32(buf_ld(rv, ov + 64 * vo), vv);
 #pragma unroll
-  for (int i = 0; i < KT; ++i) {
-    settle(dq[i]);
-    settle(as[i]);
-    settle(kept[i]);
+      for (int x = 0; x < 8; ++x) zv = fmaf((float)z[x], vv[x], zv);
+      h8_t u = {};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {  // D[j][i], of which j <= i counts
+        if (ONE && j > wv) break;
+        u = ld8(U + (vo * 4 + j) * 512);
+        s1[j] = mfma_k32(u, y, s1[j]);
+        s2[j] = mfma_k32(u, z, s2[j]);
+      }
+      if (ONE) with_states(vo, f8, y, z, u);  // (the last u is my own)
+    }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    settle(s1[j]);
+    settle(s2[j]);
   }
   __syncthreads();
   // S1, S2 masked; their largest entry, so that they can be fp16 whatever U is
-  const int i = 16 * wv + d;
   float top = 0.f;
+  const float ghi = ge[2 * C + i], glo = ge[3 * C + i];
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt)
+    {
+      const f4_t h = *(const f4_t *)&ge[2 * C + 16 * jt + 4 * g4], l = *(const f4_t *)&ge[3 * C + 16 * jt + 4 * g4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int j = 16 * jt + 4 * g4 + x;
-      const float e = exp2_((ge[2 * C + i] - ge[2 * C + j]) + (ge[3 * C + i] - ge[3 * C + j]));
-      s1[jt][x] = j <= i ? e * s1[jt][x] : 0.f;
-      s2[jt][x] = j < i ? -e * s2[jt][x] : 0.f;
-      top = fmaxf(top, fmaxf(fabsf(s1[jt][x]), fabsf(s2[jt][x])));
+      for (int x = 0; x < 4; ++x) {
+        const int j = 16 * jt + 4 * g4 + x;
+        const float e = exp2_((ghi - h[x]) + (glo - l[x]));
+        s1[jt][x] = j <= i ? e * s1[jt][x] : 0.f;
+        s2[jt][x] = j < i ? -e * s2[jt][x] : 0.f;
+        top = fmaxf(top, fmaxf(fabsf(s1[jt][x]), fabsf(s2[jt][x])));
+      }
     }
   top = group_max_nonneg<64>(top);
   zv += __shfl_xor(zv, 16, 64);
   zv += __shfl_xor(zv, 32, 64);
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) hd += __shfl_xor(hd, m, 64);
-  if (lane == 0) {
-    red[wv * 4] = top;
-    red[wv * 4 + 1] = hd;
-  }
+  if (lane == 0) red[wv * 4] = top;
   __syncthreads();
   top = fmaxf(fmaxf(red[0], red[4]), fmaxf(red[8], red[12]));
   const int ex = min(max(ilog2f(top), -100), 100);
@@ -1066,8 +1084,23 @@ __global__ void __launch_bounds__(256, 2)
     const int o = i * LC + 16 * jt + 4 * g4;
     *(u2_t *)&S1[o] = pack4_h(ss * s1[jt]);
     *(u2_t *)&S2[o] = pack4_h(ss * s2[jt]);
-    *(u2_t *)&Sb[o] = pack4_h((ss * bt) * s2[jt]);
   }
+
+  if (!ONE)
+#pragma unroll
+    for (int vb = 0; vb < V32; ++vb) {
+      const h8_t f8 = factor(vb);
+      with_states(vb, f8, bf16_to_h8(buf_ld(ry, ov + 64 * vb), sc), ld8(Z + vb * 2048) * f8, ld8(U + (vb * 4 + wv) * 512));
+    }
+#pragma unroll
+  for (int x = 0; x < KT; ++x) {
+    settle(dq[x]);
+    settle(as[x]);
+    settle(kept[x]);
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) hd += __shfl_xor(hd, m, 64);
+  if (lane == 0) red[wv * 4 + 1] = hd;
   __syncthreads();
   const bool heads = a.N != a.Nqk;
   const float inv = 1.f / sc;
@@ -1078,7 +1111,7 @@ __global__ void __launch_bounds__(256, 2)
     row1[kb] = ld8(S1 + i * LC + 32 * kb + 8 * g4);
     row2[kb] = ld8(S2 + i * LC + 32 * kb + 8 * g4);
     col1[kb] = ld8_tr(S1, LC, 32 * kb, 16 * wv);
-    colb[kb] = ld8_tr(Sb, LC, 32 * kb, 16 * wv);
+    colb[kb] = ld8_tr(S2, LC, 32 * kb, 16 * wv) * ld8(bh + 32 * kb + 8 * g4);
   }
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
@@ -1190,17 +1223,29 @@ hipError_t fwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStre
   if (!a.write_y) return fwd_go<K, VB, false, true>(a, l, w, s);
   return a.ckpt ? fwd_go<K, VB, true, true>(a, l, w, s) : fwd_go<K, VB, true, false>(a, l, w, s);
 }
+template <int K, int V32>
+hipError_t grad_go(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, int vb, hipStream_t s) {
+  constexpr int lds = lds_grad<K>();
+  const hipError_t e = set_max_lds_once(delta_half_grad_kernel<K, V32>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((delta_half_grad_kernel<K, V32>), dim3((unsigned)(a.B * a.N) * (unsigned)l.chunks), dim3(256), lds, s,
+                     a, l.chunks, vb, w.gates, (const half_t *)a.ckpt, (const half_t *)(a.ckpt + l.states), w.dstates,
+                     w.rows_z, w.scales, w.dqh, w.dkh);
+  return hipGetLastError();
+}
 template <int K, int VB>
 hipError_t bwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
-  constexpr int lds = lds_bwd<K, VB>(), ldsg = lds_grad<K>();
+  constexpr int lds = lds_bwd<K, VB>();
   hipError_t e = set_max_lds_once(delta_half_bwd_kernel<K, VB>, lds);
-  if (e == hipSuccess) e = set_max_lds_once(delta_half_grad_kernel<K>, ldsg);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((delta_half_bwd_kernel<K, VB>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a, l.chunks, w.gates, w.mats, w.dstates, w.rows_z, w.scales);
   if ((e = hipGetLastError()) != hipSuccess || l.chunks == 0) return e;
-  hipLaunchKernelGGL(delta_half_grad_kernel<K>, dim3((unsigned)(a.B * a.N) * (unsigned)l.chunks), dim3(256), ldsg, s, a, l.chunks, VB, w.gates, (const half_t *)a.ckpt,
-                     (const half_t *)(a.ckpt + l.states), w.dstates, w.rows_z, w.scales, w.dqh, w.dkh);
-  return hipGetLastError();
+  switch (a.V) {
+    case 32: return grad_go<K, 1>(a, l, w, VB, s);
+    case 64: return grad_go<K, 2>(a, l, w, VB, s);
+    case 128: return grad_go<K, 4>(a, l, w, VB, s);
+    default: return grad_go<K, 8>(a, l, w, VB, s);
+  }
 }
 template <int K>
 hipError_t fwd_k(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
