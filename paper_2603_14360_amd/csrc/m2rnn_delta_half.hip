@@ -1180,6 +1180,19 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   }
 }
 
+// dq and dk of heads that share q and k: the sums over the heads of a group, in increasing order
+__global__ void __launch_bounds__(256)
+    delta_half_heads_kernel(const float *__restrict__ dq_heads, const float *__restrict__ dk_heads, void *__restrict__ dq,
+                            void *__restrict__ dk, size_t vecs, int K4, int rep) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;  // four elements of [B T Nqk][K]
+  if (i >= vecs) return;
+  const size_t row = i / K4, c = i - row * K4;
+  const float *src = (blockIdx.y ? dk_heads : dq_heads) + (row * rep * K4 + c) * 4;
+  f4_t s = *(const f4_t *)src;
+  for (int r = 1; r < rep; ++r) s += *(const f4_t *)(src + (size_t)r * K4 * 4);
+  *(u2_t *)((unsigned short *)(blockIdx.y ? dk : dq) + 4 * i) = u2_t{pack2_bf16(s[0], s[1]), pack2_bf16(s[2], s[3])};
+}
+
 // ------------------------------------------------------------------ launches
 struct Ws {
   float *gates;
@@ -1296,10 +1309,10 @@ hipError_t delta_half_bwd(const DeltaArgs &a, hipStream_t s) {
   if (l.chunks > 0 && (e = prep<true>(a, l, w, s)) != hipSuccess) return e;
   e = a.K == 32 ? bwd_k<32>(a, l, w, s) : a.K == 64 ? bwd_k<64>(a, l, w, s) : bwd_k<128>(a, l, w, s);
   if (e != hipSuccess || l.chunks == 0 || a.N == a.Nqk) return e;
-  BwdArgs h = {};
-  h.B = a.B; h.T = a.T; h.N = a.N; h.Nqk = a.Nqk; h.K = a.K; h.io = a.io;
-  if ((e = generic_head_group_sum(h, w.dqh, a.dq, s)) != hipSuccess) return e;
-  return generic_head_group_sum(h, w.dkh, a.dk, s);
+  const size_t vecs = (size_t)a.B * a.T * a.Nqk * (a.K / 4);
+  hipLaunchKernelGGL(delta_half_heads_kernel, dim3((unsigned)((vecs + 255) / 256), 2), dim3(256), 0, s, w.dqh, w.dkh, a.dq,
+                     a.dk, vecs, a.K / 4, a.N / a.Nqk);
+  return hipGetLastError();
 }
 
 }  // namespace m2rnn

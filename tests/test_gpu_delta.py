@@ -107,6 +107,25 @@ def test_without_checkpoints(io, T, K, V, Nqk):
     check(run(s, io, backward=False), {"y": y, "HT": HT}, (io, T, K, V))
 
 
+# enough states for the workgroups with 32 columns (bf16), where the sizes above run on those with 16
+@pytest.mark.parametrize("K,V", [(K, V) for K in (32, 64, 128) for V in (32, 64, 128, 256)])
+def test_many_states(K, V):
+    T = 130 if V < 256 else 65
+    N = 4 if V < 128 else 2
+    B = -(-129 // (N * (V // 32)))
+    s = dr.rule_inputs(K * V, B, T, N, K, V, Nqk=2, io="bf16")
+    check(run(s, "bf16", use_ckpt=V != 64), dr.rule(s), (K, V))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [16, 32, 64, 128])
+@pytest.mark.parametrize("B,N,V,T", [(128, 4, 64, 1), (65, 4, 128, 3)])
+def test_many_states_step_by_step(io, K, B, N, V, T):
+    s = dr.rule_inputs(K + T, B, T, N, K, V, Nqk=1, io=io)
+    y, HT, _ = dr.rule_fwd(*(s[n] for n in ("q", "k", "v", "g", "beta", "H0")))
+    check(run(s, io, backward=False), {"y": y, "HT": HT}, (io, K, V))
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [7, 150])
 @pytest.mark.parametrize("what", ["resets", "open", "shut", "padded", "still", "strong", "same_key", "beta_two"])
