@@ -311,8 +311,9 @@ m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t group
  * k is used as it is: with beta_t |k_t|^2 <= 2 the rule does not expand, e.g. keys of unit length
  * (m2rnn_group_norm_fwd) and beta in [0, 2].  A step with g = 0 and beta = 0 leaves the state as it was: so
  * are sequences of a batch padded at their end (q, k, v of the padding finite, their y to be ignored).
- * Without checkpoints a forward of few steps runs the recurrence step by step in one launch and needs no
- * workspace (m2rnn_delta_route_string: "step"); other calls go by chunks of steps.
+ * Without checkpoints a forward of up to 12 steps (fp32: 16) runs the recurrence step by step in one launch and
+ * needs no workspace (m2rnn_delta_route_string: "step"); other calls go by chunks of steps ("chunk64<half>": 64 of
+ * them on fp16 operands, "chunk32<f32>": 32 in fp32).
  *
  * m2rnn_delta_bwd: gradients of  L = sum y * dy + sum HT * dHT.
  *   ckpt  what the forward wrote, or NULL: then the states are made again, in the workspace
@@ -320,10 +321,18 @@ m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t group
  *   dq, dk [B,T,Nqk,K] io (summed over the heads that share one)    dv [B,T,N,V] io
  *   dg, dbeta [B,T,N] io (bf16 too: the sums behind them are no finer there)
  *   dH0 [B,N,K,V] fp32, or NULL
+ *   H0 is read only where ckpt is NULL (a forward that carried its state in place has overwritten it).
  *   workspace: m2rnn_delta_workspace_bytes(desc, 0 forward | 1 backward with ckpt | 2 without).
- * Numbers: fp32 io is computed in fp32 throughout.
- * A NaN or an infinity in the inputs of a step may reach y of up to 63 steps before it (the steps of a chunk
- * are computed together), and its gradients those of the chunk.
+ *   N V and Nqk K below 2^23; B N (T / 32 + 1) below 2^24.
+ * Numbers: fp32 io is computed in fp32 throughout (and bf16 io with K = 16 or V = 16).  bf16 io feeds fp16 matrix-core
+ * operands: magnitudes of q, k, v, the state and products of two keys or of a query and a key must stay below
+ * 2*10^4; the states and dH0 are as good as fp32 with operands of 22 bits, other results carry the 11 bits that
+ * bf16 can use.  dy, dHT and the gradients may have any magnitude; of a sequence, gradients that are 2^-24 of the
+ * largest one in the same 64 steps are lost beside it.
+ * A NaN or an infinity in a step reaches y of up to 63 steps before it (the steps of a chunk are computed together,
+ * and what they do not see of each other is multiplied by zero), the states behind it, and the gradients of both;
+ * in q and k all of the head's columns, in v and dy the column's; never another head's or batch element's.
+ * The same call gives the same bits (no atomics).
  * Errors as for the scan; M2RNN_ERR_CHUNK for a chunk that is not 0.
  */
 size_t m2rnn_delta_ckpt_bytes(const m2rnn_desc *desc);

@@ -466,7 +466,9 @@ class Delta:
         return self.y, self.HT
 
     def bwd(self, q, k, v, g, beta, H0, dy, dHT=None, use_ckpt=True):
-        """dq, dk, dv, dg, dbeta (io dtype) and dH0 (fp32)."""
+        """dq, dk, dv, dg, dbeta (io dtype) and dH0 (fp32).  H0 is only read with use_ckpt=False."""
+        if not self.backward:
+            raise ValueError("made with backward=False: there is no room for gradients")
         out = (self.dq, self.dk, self.dv, self.dg, self.dbeta, self.dH0)
         ws, dev = self.workspace, self.torch._C._cuda_getDevice()
         rc = self._native.delta_bwd(ctypes.addressof(self.desc), q, k, v, g, beta, H0, self.ckpt if use_ckpt else None,

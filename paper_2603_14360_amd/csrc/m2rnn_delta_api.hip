@@ -15,9 +15,9 @@ m2rnn_status check(const m2rnn_desc *d) {
   const auto dim = [](int x) { return x == 16 || x == 32 || x == 64 || x == 128; };
   if (!dim(d->K) || !(dim(d->V) || d->V == 256) || d->flags != 0) return M2RNN_ERR_SHAPE;
   if ((double)d->B * (d->T > 0 ? d->T : 1) * d->N * d->K * d->V > 1e15) return M2RNN_ERR_SHAPE;
-  // (units, and units times parts or chunks, are workgroup numbers)
-  const double units = (double)d->B * d->N;
-  if (units * 16 > 1e9 || units * (d->T / 32 + 1) > 2e9) return M2RNN_ERR_SHAPE;
+  // (units times parts or chunks are workgroups of 256 threads, of which a launch has fewer than 2^32)
+  const double units = (double)d->B * d->N, most = (1 << 24) - 1;
+  if (units * 16 > most || units * (d->T / 32 + 1) > most) return M2RNN_ERR_SHAPE;
   // (a chunk's rows are reached by 31-bit byte offsets)
   if ((double)d->N * d->V >= (1 << 23) || (double)d->Nqk * d->K >= (1 << 23)) return M2RNN_ERR_SHAPE;
   if (d->chunk != 0) return M2RNN_ERR_CHUNK;
@@ -56,7 +56,7 @@ size_t m2rnn_delta_workspace_bytes(const m2rnn_desc *desc, int bwd) {
 
 const char *m2rnn_delta_route_string(const m2rnn_desc *desc, int bwd) {
   if (check(desc) != M2RNN_OK) return "invalid descriptor";
-  if (!bwd && delta_step_serves(desc->T)) return "step";
+  if (!bwd && delta_step_serves(desc->T, desc->io)) return "step";
   return half(args_of(desc)) ? "chunk64<half>" : "chunk32<f32>";
 }
 
@@ -72,7 +72,7 @@ m2rnn_status m2rnn_delta_fwd(const m2rnn_desc *desc, const void *q, const void *
   DeltaArgs a = args_of(desc);
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.H0 = H0; a.y = y; a.HT = HT;
   a.ckpt = (char *)ckpt; a.ws = (char *)workspace;
-  const bool step = !ckpt && delta_step_serves(desc->T);
+  const bool step = !ckpt && delta_step_serves(desc->T, desc->io);
   const size_t need = step ? 0 : ws_bytes(layout(a), 0);
   if (need > 0 && (!workspace || workspace_bytes < need)) return workspace ? M2RNN_ERR_WORKSPACE : M2RNN_ERR_NULL;
   if (desc->B == 0) return M2RNN_OK;

@@ -1184,13 +1184,13 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
 __global__ void __launch_bounds__(256)
     delta_half_heads_kernel(const float *__restrict__ dq_heads, const float *__restrict__ dk_heads, void *__restrict__ dq,
                             void *__restrict__ dk, size_t vecs, int K4, int rep) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;  // four elements of [B T Nqk][K]
-  if (i >= vecs) return;
-  const size_t row = i / K4, c = i - row * K4;
-  const float *src = (blockIdx.y ? dk_heads : dq_heads) + (row * rep * K4 + c) * 4;
-  f4_t s = *(const f4_t *)src;
-  for (int r = 1; r < rep; ++r) s += *(const f4_t *)(src + (size_t)r * K4 * 4);
-  *(u2_t *)((unsigned short *)(blockIdx.y ? dk : dq) + 4 * i) = u2_t{pack2_bf16(s[0], s[1]), pack2_bf16(s[2], s[3])};
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < vecs; i += (size_t)gridDim.x * 256) {
+    const size_t row = i / K4, c = i - row * K4;  // four elements of [B T Nqk][K]
+    const float *src = (blockIdx.y ? dk_heads : dq_heads) + (row * rep * K4 + c) * 4;
+    f4_t s = *(const f4_t *)src;
+    for (int r = 1; r < rep; ++r) s += *(const f4_t *)(src + (size_t)r * K4 * 4);
+    *(u2_t *)((unsigned short *)(blockIdx.y ? dk : dq) + 4 * i) = u2_t{pack2_bf16(s[0], s[1]), pack2_bf16(s[2], s[3])};
+  }
 }
 
 // ------------------------------------------------------------------ launches
@@ -1211,8 +1211,12 @@ Ws carve(const DeltaLayout &l, char *p) {
   return w;
 }
 
-// Columns of V per workgroup of the kernels that run in order
-int columns(const DeltaArgs &a) { return a.B * a.N * (a.V / 32) <= 128 ? 16 : 32; }
+// Columns of V per workgroup of the kernels that run in order: 32, or 16 where that leaves half of the 256 CUs
+// without one.  us, forward / backward kernel, 32 -> 16 columns: 32 states of 128 x 128, 8192 steps 333 / 467 ->
+// 277 / 403 (128 workgroups of 32 columns); 128 of 64 x 64, 4096 steps 163 / 231 -> 230 / 260 (256).
+int columns(const DeltaArgs &a) {
+  return a.B * a.N * (a.V / 32) <= 128 ? 16 : 32;
+}
 
 template <bool BWD>
 hipError_t prep(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
@@ -1310,7 +1314,8 @@ hipError_t delta_half_bwd(const DeltaArgs &a, hipStream_t s) {
   e = a.K == 32 ? bwd_k<32>(a, l, w, s) : a.K == 64 ? bwd_k<64>(a, l, w, s) : bwd_k<128>(a, l, w, s);
   if (e != hipSuccess || l.chunks == 0 || a.N == a.Nqk) return e;
   const size_t vecs = (size_t)a.B * a.T * a.Nqk * (a.K / 4);
-  hipLaunchKernelGGL(delta_half_heads_kernel, dim3((unsigned)((vecs + 255) / 256), 2), dim3(256), 0, s, w.dqh, w.dkh, a.dq,
+  const size_t blocks = (vecs + 255) / 256;
+  hipLaunchKernelGGL(delta_half_heads_kernel, dim3((unsigned)(blocks < (1u << 20) ? blocks : 1u << 20), 2), dim3(256), 0, s, w.dqh, w.dkh, a.dq,
                      a.dk, vecs, a.K / 4, a.N / a.Nqk);
   return hipGetLastError();
 }

@@ -32,7 +32,8 @@ def bwd(d, q=A, k=A, v=A, g=A, beta=A, H0=None, ckpt=A, dy=A, dHT=None, dq=A, dk
 
 BAD = [(dict(K=24), 2), (dict(K=256), 2), (dict(V=48), 2), (dict(V=512), 2), (dict(N=0), 2), (dict(Nqk=3), 2),
        (dict(Nqk=0), 2), (dict(B=-1), 2), (dict(T=-1), 2), (dict(io=5), 3), (dict(flags=1), 2), (dict(chunk=16), 7),
-       (dict(B=1 << 30, N=1 << 20), 2), (dict(B=1 << 20, N=64, T=1 << 20), 2)]
+       (dict(B=1 << 30, N=1 << 20), 2), (dict(B=1 << 20, N=64, T=1 << 20), 2), (dict(B=1, N=64, T=1 << 25), 2),
+       (dict(N=1 << 18, Nqk=1), 2)]
 
 
 @pytest.mark.parametrize("kw,code", BAD)
