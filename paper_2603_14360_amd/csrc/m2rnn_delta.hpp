@@ -49,6 +49,7 @@ struct DeltaArgs {
 // Sizes in bytes (multiples of 256) of the parts of the scratch and of the checkpoints of a chunked call.
 struct DeltaLayout {
   int C, chunks;
+  bool kept;      // gates, T and P are kept with the checkpoints
   size_t gates;   // per unit and chunk: e^G, e^{G_C - G}, and G / ln 2 as a sum of two floats, C each
   size_t mats;    // T and P of every chunk
   size_t states;  // one state per chunk

@@ -60,6 +60,19 @@ __global__ void __launch_bounds__(256, 2) delta_prep_kernel(DeltaArgs a, int chu
   const int t0 = ch * C, lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float *gt = gates + (size_t)blockIdx.x * 4 * C;
   float *Tm = mats + (size_t)blockIdx.x * 2 * C * C, *Pm = Tm + C * C;
+  // tile (r, c) of K K^T and of Q K^T: wave 2 r + c
+  const int r = wv >> 1, c = wv & 1, l16 = lane & 15, g4 = lane >> 4;
+  const size_t row = (size_t)a.Nqk * a.K, base = ((size_t)b * a.T + t0) * row + (size_t)nq * a.K + 4 * g4;
+  const int ti = 16 * r + l16, tj = 16 * c + l16;
+  const bool iok = t0 + ti < a.T, jok = t0 + tj < a.T;
+  f4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
+  for (int e = 0; e < a.K; e += 16) {  // D[j][i] with A = rows j: a lane holds four j of one i
+    const f4_t kj = load4<IO>(a.k, base + tj * row + e, jok);
+    kk = mma(kj, load4<IO>(a.k, base + ti * row + e, iok), kk);
+    qk = mma(kj, load4<IO>(a.q, base + ti * row + e, iok), qk);
+  }
+  settle(kk);
+  settle(qk);
   if (wv == 0) {
     const bool in = lane < C && t0 + lane < a.T;
     const size_t e = ((size_t)b * a.T + (in ? t0 + lane : 0)) * a.N + n;
@@ -76,19 +89,6 @@ __global__ void __launch_bounds__(256, 2) delta_prep_kernel(DeltaArgs a, int chu
     }
   }
   __syncthreads();
-  // tile (r, c) of K K^T and of Q K^T: wave 2 r + c
-  const int r = wv >> 1, c = wv & 1, l16 = lane & 15, g4 = lane >> 4;
-  const size_t row = (size_t)a.Nqk * a.K, base = ((size_t)b * a.T + t0) * row + (size_t)nq * a.K + 4 * g4;
-  const int ti = 16 * r + l16, tj = 16 * c + l16;
-  const bool iok = t0 + ti < a.T, jok = t0 + tj < a.T;
-  f4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
-  for (int e = 0; e < a.K; e += 16) {  // D[j][i] with A = rows j: a lane holds four j of one i
-    const f4_t kj = load4<IO>(a.k, base + tj * row + e, jok);
-    kk = mma(kj, load4<IO>(a.k, base + ti * row + e, iok), kk);
-    qk = mma(kj, load4<IO>(a.q, base + ti * row + e, iok), qk);
-  }
-  settle(kk);
-  settle(qk);
   f4_t p;
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
@@ -602,11 +602,15 @@ __global__ void __launch_bounds__(256, 2)
 constexpr int lds_grad(int K) { return (2 * K * LC + 4 * C * LC + 5 * C + 9 * C + 8) * 4; }
 
 // ------------------------------------------------------------------ launches
-Ws carve(const DeltaLayout &l, char *p) {
+// Gates, T and P stand behind the states and U of the checkpoints where there are any (the backward takes them from
+// there), else in the workspace.
+Ws carve(const DeltaLayout &l, char *p, char *ckpt) {
   Ws w;
-  w.gates = (float *)p;
-  w.mats = (float *)(p += l.gates);
-  w.states = (float *)(p += l.mats);
+  char *m = ckpt ? ckpt + l.states + l.rows : p;
+  w.gates = (float *)m;
+  w.mats = (float *)(m + l.gates);
+  p += l.gates + l.mats;
+  w.states = (float *)p;
   w.rows = (float *)(p += l.states);
   w.dqh = (float *)(p += l.rows);
   w.dkh = (float *)(p += l.heads);
@@ -651,7 +655,7 @@ hipError_t back(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream
 template <typename IO>
 hipError_t fwd_t(const DeltaArgs &a, hipStream_t s) {
   const DeltaLayout l = delta_f32_layout(a);
-  const Ws w = carve(l, a.ws);
+  const Ws w = carve(l, a.ws, a.ckpt);
   hipError_t e = l.chunks > 0 ? prep<IO>(a, l, w, s) : hipSuccess;
   if (e != hipSuccess) return e;
   M2RNN_DELTA_K(scan, a, l, w, s)
@@ -660,13 +664,13 @@ hipError_t fwd_t(const DeltaArgs &a, hipStream_t s) {
 template <typename IO>
 hipError_t bwd_t(const DeltaArgs &a, hipStream_t s) {
   const DeltaLayout l = delta_f32_layout(a);
-  const Ws w = carve(l, a.ws);
-  hipError_t e = l.chunks > 0 ? prep<IO>(a, l, w, s) : hipSuccess;
-  if (e != hipSuccess) return e;
+  const Ws w = carve(l, a.ws, a.ckpt);
+  hipError_t e = hipSuccess;
   if (a.own_ckpt && l.chunks > 0) {
     DeltaArgs f = a;
     f.write_y = 0;
     f.HT = nullptr;
+    if ((e = prep<IO>(a, l, w, s)) != hipSuccess) return e;
     M2RNN_DELTA_K(scan, f, l, w, s)
     if (e != hipSuccess) return e;
   }
@@ -684,6 +688,7 @@ hipError_t bwd_t(const DeltaArgs &a, hipStream_t s) {
 DeltaLayout delta_f32_layout(const DeltaArgs &a) {
   DeltaLayout l;
   l.C = C;
+  l.kept = true;
   l.chunks = ceil_div(a.T, C);
   const size_t n = (size_t)a.B * a.N * l.chunks, steps = (size_t)a.B * a.T * a.N;
   l.gates = align256(n * 4 * C * sizeof(float));

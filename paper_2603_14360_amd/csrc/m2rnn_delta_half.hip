@@ -1284,6 +1284,7 @@ bool delta_half_serves(int K, int V, int io) { return io == 1 && K >= 32 && V >=
 DeltaLayout delta_half_layout(const DeltaArgs &a) {
   DeltaLayout l;
   l.C = C;
+  l.kept = false;
   l.chunks = ceil_div(a.T, C);
   const size_t n = (size_t)a.B * a.N * l.chunks, steps = (size_t)a.B * a.T * a.N;
   l.gates = align256(n * kGates * sizeof(float));
