@@ -1,7 +1,7 @@
 // Gated delta rule, chunks of 32 steps, everything in fp32 on the fp32 matrix instructions (16x16x4): the
 // kernels of fp32 io.  The lines of the rule by chunks stand in m2rnn_delta.hpp.
 //
-//   delta_prep_kernel   one workgroup per chunk: gates, T and P                     -> workspace
+//   delta_prep_kernel   one workgroup per chunk: gates, T and P                     -> checkpoints or workspace
 //   delta_fwd_kernel    one workgroup per state and 16 columns of V, chunks in order -> y, HT, (H, U)
 //   delta_bwd_kernel    the same, backwards                                          -> dv, dH0, dH and Z
 //   delta_grad_kernel   one workgroup per chunk: S1, S2 and what follows             -> dq, dk, dg, dbeta
@@ -11,7 +11,11 @@
 // instructions, and of D it holds rows 4 (lane / 16) .. + 3 of column lane % 16.  Which of two factors is A is
 // free; it is chosen so that those four are neighbours where D goes next.
 //
-// Chunks of 32 and not 64, because q, k and their transposes of a chunk lie in LDS: 100 KB at K = 128.
+// Chunks of 32 and not 64, because q, k and their transposes of a chunk lie in LDS: 81 KB at K = 128.
+//
+// What bounds them is the latency of a chunk's dependent products; 16 columns a workgroup make the chains as many as
+// there can be.  4 x 512 steps, 8 heads of 32 x 32, fp32: T and P 9 us, forward 24, backward 31 (1.5 and 1.9 a chunk on
+// 64 workgroups), gradients 12.
 #include "m2rnn_delta.hpp"
 
 namespace m2rnn {

