@@ -282,7 +282,7 @@ m2rnn_status m2rnn_gated_rmsnorm_bwd(int32_t B, int32_t T, int32_t D, int32_t io
  *   x, out, dout, dx, a, da [B,T,D] io; a NULL: no gate.   w, b [D] io; NULL: 1, 0.
  *   dw, db [D] fp32: gradients of w and b (of a w of ones, a b of zeros where those are NULL),
  *   overwritten, summed over (b, t) in a fixed order; NULL: not wanted.
- *   mode: M2RNN_NORM_* or'ed.   L: a multiple of 8, at most 1024.   eps >= 0.
+ *   mode: M2RNN_NORM_* or'ed.   L: a multiple of 8, at most 1024.   D below 2^30.   eps >= 0.
  *   workspace: m2rnn_group_norm_workspace_bytes(B, T, D) bytes, for dw and db only.
  *   out may be x or a, dx may be x or dout, da may be a or dout or x, as long as no two outputs are
  *   the same buffer: a token's inputs are read before its outputs are written.

@@ -484,6 +484,7 @@ static m2rnn_status check_group_norm(int32_t B, int32_t T, int32_t D, int32_t gr
   if (st != M2RNN_OK) return st;
   if (groups < 1 || D % groups != 0 || (D / groups) % 8 != 0 || D / groups > group_norm_max_group() || !(eps >= 0.f))
     return M2RNN_ERR_SHAPE;
+  if (D >= (1 << 30)) return M2RNN_ERR_SHAPE;  // (the sums of dw and db count 2 D columns in an int)
   if ((mode & ~(M2RNN_NORM_CENTER | M2RNN_NORM_SILU)) != 0 || ((mode & M2RNN_NORM_SILU) && a)) return M2RNN_ERR_SHAPE;
   return M2RNN_OK;
 }
@@ -499,7 +500,7 @@ static GroupNormArgs group_norm_args(int32_t B, int32_t T, int32_t D, int32_t gr
 }
 
 size_t m2rnn_group_norm_workspace_bytes(int32_t B, int32_t T, int32_t D) {
-  return check_block(B, T, D, M2RNN_F32) == M2RNN_OK ? group_norm_scratch_bytes(B, T, D) : 0;
+  return check_block(B, T, D, M2RNN_F32) == M2RNN_OK && D < (1 << 30) ? group_norm_scratch_bytes(B, T, D) : 0;
 }
 
 m2rnn_status m2rnn_group_norm_fwd(int32_t B, int32_t T, int32_t D, int32_t groups, int32_t io, int32_t mode,

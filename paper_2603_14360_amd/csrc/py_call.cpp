@@ -253,6 +253,10 @@ PyObject *call_group_norm_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (!ready((const void *)group_norm_fwd) || !arity(n, 9) || !shape_of(args[0], s, io, dev)) return nullptr;
   const long groups = PyLong_AsLong(args[4]), mode = PyLong_AsLong(args[6]);
   const double eps = PyFloat_AsDouble(args[5]);
+  if (!PyErr_Occurred() && (groups != (int32_t)groups || mode != (int32_t)mode)) {
+    PyErr_SetString(PyExc_ValueError, "groups or mode is too large");
+    return nullptr;
+  }
   void *x, *a, *w, *b, *out, *stream;
   const int64_t all = (int64_t)s[0] * s[1] * s[2];
   const at::ScalarType t = io_type(io);

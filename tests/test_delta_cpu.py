@@ -155,3 +155,18 @@ def test_tensors_that_are_not_on_the_gpu_are_refused():
         mb._call().delta_bwd(*args, None, A, A, None, A, A, A, A, A, A, A, 0, 1 << 40, -1)
     with pytest.raises(TypeError):
         mb._call().delta_fwd(*args)
+
+
+def test_a_norm_of_more_channels_than_its_sums_can_count_is_refused():
+    L, p = mb.lib(), ctypes.c_void_p(A)
+    D = 1 << 30
+    assert L.m2rnn_group_norm_fwd(1, 1, D, D // 8, 1, 0, p, None, p, p, 1e-5, p, None) == 2
+    assert L.m2rnn_group_norm_bwd(1, 1, D, D // 8, 1, 0, p, None, p, p, 1e-5, p, p, None, p, p, p, 1 << 60, None) == 2
+    assert mb.m2rnn_group_norm_workspace_bytes(1, 1, D) == 0
+
+
+def test_a_count_beyond_32_bits_is_not_cut_to_one_that_fits():
+    x = cpu(2, 3, 16)
+    for groups, mode in (((1 << 32) + 2, 0), (2, 1 << 32), (-(1 << 32) + 2, 0)):
+        with pytest.raises(ValueError, match="too large"):
+            mb.m2rnn_group_norm_fwd(x, None, cpu(16), None, groups, 1e-5, mode, x)
