@@ -320,14 +320,15 @@ m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t group
  *   dy [B,T,N,V] io    dHT [B,N,K,V] fp32 or NULL (zero)
  *   dq, dk [B,T,Nqk,K] io (summed over the heads that share one)    dv [B,T,N,V] io
  *   dg, dbeta [B,T,N] io (bf16 too: the sums behind them are no finer there)
- *   dH0 [B,N,K,V] fp32, or NULL
+ *   dH0 [B,N,K,V] fp32, or NULL; may be dHT (segments of a sequence, from the last to the first)
  *   H0 is read only where ckpt is NULL (a forward that carried its state in place has overwritten it).
  *   workspace: m2rnn_delta_workspace_bytes(desc, 0 forward | 1 backward with ckpt | 2 without).
  *   N V and Nqk K below 2^23; B N (T / 32 + 1) below 2^24.
  * Numbers: fp32 io is computed in fp32 throughout (and bf16 io with K = 16 or V = 16).  bf16 io feeds fp16 matrix-core
  * operands: magnitudes of q, k, v, the state and products of two keys or of a query and a key must stay below
  * 2*10^4; the states and dH0 are as good as fp32 with operands of 22 bits, other results carry the 11 bits that
- * bf16 can use.  dy, dHT and the gradients may have any magnitude; of a sequence, gradients that are 2^-24 of the
+ * bf16 can use; what is smaller than 2^-14 is held to some 2^-25 of one, not of itself (v and states all below 10^-4
+ * are better scaled up, or passed as fp32).  dy, dHT and the gradients may have any magnitude; of a sequence, gradients that are 2^-24 of the
  * largest one in the same 64 steps are lost beside it.
  * A NaN or an infinity in a step reaches y of up to 63 steps before it (the steps of a chunk are computed together,
  * and what they do not see of each other is multiplied by zero), the states behind it, and the gradients of both;
