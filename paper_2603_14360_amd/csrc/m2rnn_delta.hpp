@@ -52,6 +52,7 @@ struct DeltaLayout {
   bool kept;      // gates, T and P are kept with the checkpoints
   size_t gates;   // per unit and chunk: e^G, e^{G_C - G}, and G / ln 2 as a sum of two floats, C each
   size_t mats;    // T and P of every chunk
+  size_t carry;   // the states between the launches of a forward (0: there is one)
   size_t states;  // one state per chunk
   size_t rows;    // U or Z of every step
   size_t scales;  // powers of two of the gradients (0: none)

@@ -2,7 +2,8 @@
 // chunks stand in m2rnn_delta.hpp.
 //
 //   delta_half_prep_kernel   one workgroup per chunk: gates, T and P             -> workspace
-//   delta_half_fwd_kernel    one workgroup per state and VB columns of V, chunks in order -> y, HT, (H, U)
+//   delta_half_fwd_kernel    one workgroup per state and VB columns of V, chunks in order -> y, HT, (H, U); few long
+//                            sequences in several launches, T and P of the next one's chunks beside them
 //   delta_half_bwd_kernel    the same, backwards                                  -> dv, dH0, dH and Z
 //   delta_half_grad_kernel   one workgroup per chunk                              -> dq, dk, dg, dbeta
 //
@@ -19,6 +20,8 @@
 // What one kernel hands to another (T, P, H, U, dH, Z) is stored as the operands that the reader needs, 16 bytes
 // a lane, 1 KB an operand: no reader goes through LDS for it.
 #include "m2rnn_delta.hpp"
+
+#include <algorithm>
 
 namespace m2rnn {
 namespace {
@@ -102,13 +105,17 @@ __device__ __forceinline__ f4_t mma_f32(f4_t a, f4_t b, f4_t c) {
 // whose products run on the fp32 matrix instructions; T takes the place of A in LDS block by block.
 // What bounds it is latency: all loads are issued at once, and 24 KB of LDS leave room for six workgroups per CU.
 // 8 x 4096 steps, 16 heads of 64 x 64: 65 us forward, 98 backward (3.5 TB/s, mostly of T and P).
+struct PrepLds {
+  float As[C][C + 4], Xt[C / 2][C / 2 + 4], hi[C], lo[C], be[C];
+};
 template <int K, bool BWD>
-__global__ void __launch_bounds__(256, BWD && K == 128 ? 3 : 4)
-    delta_half_prep_kernel(DeltaArgs a, int chunks, float *__restrict__ gates, half_t *__restrict__ mats) {
+__device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int unit, int ch, float *gates, half_t *mats,
+                                           PrepLds &lds) {
   constexpr int LA = C + 4, KB = K / 32;
-  __shared__ __align__(16) float As[C][LA], Xt[C / 2][C / 2 + 4];
-  __shared__ float hi[C], lo[C], be[C];
-  const int unit = blockIdx.x / chunks, ch = blockIdx.x - unit * chunks;
+  auto &As = lds.As;
+  auto &Xt = lds.Xt;
+  float *hi = lds.hi, *lo = lds.lo, *be = lds.be;
+  const size_t slot = (size_t)unit * chunks + ch;
   const int b = unit / a.N, n = unit - b * a.N, nq = n / (a.N / a.Nqk);
   const int t0 = ch * C, lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int d = lane & 15, g4 = lane >> 4;
@@ -139,7 +146,7 @@ __global__ void __launch_bounds__(256, BWD && K == 128 ? 3 : 4)
     hi[lane] = G.hi;
     lo[lane] = G.lo;
     be[lane] = beta;
-    float *gt = gates + (size_t)blockIdx.x * kGates;
+    float *gt = gates + slot * kGates;
     gt[lane] = BWD ? exp2_((G.hi - floorf(__shfl(G.hi, 0, 64))) + G.lo) : exp2_(G.hi) * exp2_(G.lo);
     gt[C + lane] = exp2_((ghi - G.hi) + (glo - G.lo));
     gt[2 * C + lane] = G.hi;
@@ -242,7 +249,7 @@ __global__ void __launch_bounds__(256, BWD && K == 128 ? 3 : 4)
     put(32 + 16 * r + 4 * g4, 16 * c + d, x);
   }
   __syncthreads();
-  half_t *Tm = mats + (size_t)blockIdx.x * 2 * kMat, *Pm = Tm + kMat;
+  half_t *Tm = mats + slot * 2 * kMat, *Pm = Tm + kMat;
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     if (BWD ? (kb == 0 && wv >= 2) : (kb == 1 && wv < 2)) continue;  // (zero)
@@ -262,6 +269,14 @@ __global__ void __launch_bounds__(256, BWD && K == 128 ? 3 : 4)
     *(u4_t *)(Pm + mat_at(wv, kb, 0) + lane * 8) = join(ph[2 * kb], ph[2 * kb + 1]);
     if (BWD) *(u4_t *)(Pm + mat_at(wv, kb, 1) + lane * 8) = join(pl[2 * kb], pl[2 * kb + 1]);
   }
+}
+// the chunks c0 .. c1 - 1 of all units
+template <int K, bool BWD>
+__global__ void __launch_bounds__(256, BWD && K == 128 ? 3 : 4)
+    delta_half_prep_kernel(DeltaArgs a, int chunks, int c0, int c1, float *__restrict__ gates, half_t *__restrict__ mats) {
+  __shared__ __align__(16) PrepLds lds;
+  const int n = c1 - c0, unit = blockIdx.x / n;
+  prep_chunk<K, BWD>(a, chunks, unit, c0 + (int)blockIdx.x - unit * n, gates, mats, lds);
 }
 
 // ------------------------------------------------------------------ the kernels that run in order
@@ -382,18 +397,32 @@ struct Turn {
 template <int K, int VB>
 constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4; }
 
+// What a launch of the forward does: the chunks c0 .. c1 - 1 of all states, from H0 to HT, in its first `scans`
+// workgroups, and T and P of the chunks c1 .. c2 - 1, which the next launch reads, in the others.
+struct Part {
+  int c0, c1, c2;
+  unsigned scans;
+  const float *H0;
+  float *HT;
+};
 // Y: y is wanted;  CKPT: the chunks' states and U are.  8 x 4096 steps, 16 heads of 64 x 64: 163 us, 2.5 a chunk on
 // 256 workgroups (3.5 TB/s); 65 536 steps, 32 of 64 x 64 without checkpoints: 1.33 a chunk on 128 of them.
 template <int K, int VB, bool Y, bool CKPT>
 __global__ void __launch_bounds__(256, 2)
-    delta_half_fwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const half_t *__restrict__ mats,
-                          half_t *__restrict__ states, half_t *__restrict__ rows_u) {
+    delta_half_fwd_kernel(DeltaArgs a, int chunks, Part p, float *gates, half_t *mats, half_t *__restrict__ states,
+                          half_t *__restrict__ rows_u) {
   using S = Scan<K, VB>;
   constexpr int KB = S::KB, KT = S::KT, VT = S::VT, KTW = S::KTW, VTW = S::VTW, LK = S::LK;
   extern __shared__ __align__(16) char lds[];
   half_t *ks = (half_t *)lds, *Ht = ks + C * LK, *Hl = Ht + VB * LK, *Rt = Hl + VB * LK, *Rl = Rt + VB * LC;
   half_t *Ut = Rl + VB * LC, *Wt = Ut + VB * LC, *Wl = Wt + VB * LC, *turn = Wl + VB * LC;
   int unit, part;
+  if (blockIdx.x >= p.scans) {
+    const int i = blockIdx.x - p.scans, n = p.c2 - p.c1;
+    unit = i / n;
+    prep_chunk<K, false>(a, chunks, unit, p.c1 + i - unit * n, gates, mats, *(PrepLds *)lds);
+    return;
+  }
   if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int d = lane & 15, g4 = lane >> 4;
@@ -415,7 +444,7 @@ __global__ void __launch_bounds__(256, 2)
     for (int j = 0; j < VTW; ++j)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        H[i][j][x] = a.H0 ? a.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
+        H[i][j][x] = p.H0 ? p.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
   // The next chunk's, in the order of their use: k, v and gates in its first product, T in its second, q and P last.
   // Each load is issued behind the last use of its registers and so has most of a chunk to arrive.
   u4_t nk[KB], nq[KB], nv;
@@ -468,15 +497,15 @@ __global__ void __launch_bounds__(256, 2)
         }
   };
   put_state();
-  if (chunks > 0) {
-    fetch1(0);
-    fetch2(0);
-    if (Y) fetch3(0);
+  if (p.c0 < p.c1) {
+    fetch1(p.c0);
+    fetch2(p.c0);
+    if (Y) fetch3(p.c0);
     take1();
   }
   const int w = place(wv);
-  for (int ch = 0; ch < chunks; ++ch) {
-    const int next = min(ch + 1, chunks - 1);
+  for (int ch = p.c0; ch < p.c1; ++ch) {
+    const int next = min(ch + 1, p.c1 - 1);
     lds_barrier();  // the state is there, and k of the chunk before has been read
     // R = beta (v - e^G K H): D[step][column]
     h8_t hh[VT][KB], hl[VT][KB];
@@ -619,14 +648,14 @@ __global__ void __launch_bounds__(256, 2)
       *(h8_t *)(rows_u + at * C * a.V + frag_at<VB>(part, 4, wv)) = us;
     }
   }
-  if (a.HT && S::on(wv))
+  if (p.HT && S::on(wv))
 #pragma unroll
     for (int i = 0; i < KTW; ++i)
 #pragma unroll
       for (int j = 0; j < VTW; ++j)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          a.HT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] = H[i][j][x];
+          p.HT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] = H[i][j][x];
 }
 
 // Backward, chunks in reverse order.  Gradients of a chunk are brought near one by s, a power of two from the
@@ -1198,7 +1227,7 @@ __global__ void __launch_bounds__(256)
 
 // ------------------------------------------------------------------ launches
 struct Ws {
-  float *gates;
+  float *gates, *carry;
   half_t *mats, *dstates, *rows_z;
   float *scales, *dqh, *dkh;
 };
@@ -1206,7 +1235,8 @@ Ws carve(const DeltaLayout &l, char *p) {
   Ws w;
   w.gates = (float *)p;
   w.mats = (half_t *)(p += l.gates);
-  w.dstates = (half_t *)(p += l.mats);
+  w.carry = (float *)(p += l.mats);
+  w.dstates = (half_t *)(p += l.carry);
   w.rows_z = (half_t *)(p += l.states);
   w.scales = (float *)(p += l.rows);
   w.dqh = (float *)(p += l.scales);
@@ -1220,23 +1250,46 @@ Ws carve(const DeltaLayout &l, char *p) {
 int columns(const DeltaArgs &a) {
   return a.B * a.N * (a.V / 32) <= 128 ? 16 : 32;
 }
+// Chunks per launch of the forward.  Where its chains have no more than half of the CUs, a long one goes in parts whose
+// launches also form T and P of the next part, on the idle CUs: in parts of about 1024 chunks over all states, as many
+// as run at once (longer ones keep the chains' CUs busy as well), and of 16 each at least, for a launch's 6 us.
+// us, whole -> parts of half, once, twice as many: 65 536 steps of 32 states 64 x 64 1648 -> 1537, 1413, 1548; 32 768 of
+// 16 of 64 x 128 646 -> 612, 586, 621; of 8 of 128 x 128 852 -> 835, 816, -.  With chains on all 256 CUs there is
+// nothing to gain (8 x 4096 steps, 16 of 64 x 64: 231 -> 228 to 241).
+int part_chunks(const DeltaArgs &a, int chunks) {
+  const int units = a.B * a.N;
+  if (units == 0 || units * (a.V / columns(a)) > 128) return chunks;
+  return std::min(chunks, std::max(16, 1024 / units));
+}
 
 template <bool BWD>
-hipError_t prep(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
-  const dim3 grid((unsigned)(a.B * a.N) * (unsigned)l.chunks);
-  if (a.K == 32) hipLaunchKernelGGL((delta_half_prep_kernel<32, BWD>), grid, dim3(256), 0, s, a, l.chunks, w.gates, w.mats);
-  else if (a.K == 64) hipLaunchKernelGGL((delta_half_prep_kernel<64, BWD>), grid, dim3(256), 0, s, a, l.chunks, w.gates, w.mats);
-  else hipLaunchKernelGGL((delta_half_prep_kernel<128, BWD>), grid, dim3(256), 0, s, a, l.chunks, w.gates, w.mats);
+hipError_t prep(const DeltaArgs &a, const DeltaLayout &l, int c0, int c1, const Ws &w, hipStream_t s) {
+  const dim3 grid((unsigned)(a.B * a.N) * (unsigned)(c1 - c0));
+  if (a.K == 32) hipLaunchKernelGGL((delta_half_prep_kernel<32, BWD>), grid, dim3(256), 0, s, a, l.chunks, c0, c1, w.gates, w.mats);
+  else if (a.K == 64) hipLaunchKernelGGL((delta_half_prep_kernel<64, BWD>), grid, dim3(256), 0, s, a, l.chunks, c0, c1, w.gates, w.mats);
+  else hipLaunchKernelGGL((delta_half_prep_kernel<128, BWD>), grid, dim3(256), 0, s, a, l.chunks, c0, c1, w.gates, w.mats);
   return hipGetLastError();
 }
 template <int K, int VB, bool Y, bool CKPT>
 hipError_t fwd_go(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
-  constexpr int lds = lds_fwd<K, VB>();
-  const hipError_t e = set_max_lds_once(delta_half_fwd_kernel<K, VB, Y, CKPT>, lds);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((delta_half_fwd_kernel<K, VB, Y, CKPT>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a,
-                     l.chunks, w.gates, w.mats, (half_t *)a.ckpt, a.ckpt ? (half_t *)(a.ckpt + l.states) : nullptr);
-  return hipGetLastError();
+  constexpr int lds = std::max<int>(lds_fwd<K, VB>(), sizeof(PrepLds));
+  hipError_t e = set_max_lds_once(delta_half_fwd_kernel<K, VB, Y, CKPT>, lds);
+  const int step = part_chunks(a, l.chunks);
+  if (e == hipSuccess && l.chunks > 0) e = prep<false>(a, l, 0, step, w, s);
+  Part p = {0, 0, 0, delta_grid(a.B * a.N, a.V / VB), a.H0, nullptr};
+  do {
+    if (e != hipSuccess) return e;
+    p.c1 = std::min(p.c0 + step, l.chunks);
+    p.c2 = std::min(p.c1 + step, l.chunks);
+    p.HT = p.c1 < l.chunks ? w.carry : a.HT;
+    hipLaunchKernelGGL((delta_half_fwd_kernel<K, VB, Y, CKPT>), dim3(p.scans + (unsigned)(a.B * a.N) * (unsigned)(p.c2 - p.c1)),
+                       dim3(256), lds, s, a, l.chunks, p, w.gates, w.mats, (half_t *)a.ckpt,
+                       a.ckpt ? (half_t *)(a.ckpt + l.states) : nullptr);
+    e = hipGetLastError();
+    p.c0 = p.c1;
+    p.H0 = w.carry;
+  } while (p.c0 < l.chunks);
+  return e;
 }
 template <int K, int VB>
 hipError_t fwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStream_t s) {
@@ -1292,6 +1345,7 @@ DeltaLayout delta_half_layout(const DeltaArgs &a) {
   const size_t n = (size_t)a.B * a.N * l.chunks, steps = (size_t)a.B * a.T * a.N;
   l.gates = align256(n * kGates * sizeof(float));
   l.mats = align256(n * 2 * kMat * sizeof(half_t));
+  l.carry = part_chunks(a, l.chunks) < l.chunks ? align256((size_t)a.B * a.N * a.K * a.V * sizeof(float)) : 0;
   l.states = align256(n * a.K * a.V * sizeof(half_t));
   l.rows = align256(n * C * a.V * sizeof(half_t));
   l.scales = align256(n * (a.V / 16) * sizeof(float));
@@ -1301,8 +1355,7 @@ DeltaLayout delta_half_layout(const DeltaArgs &a) {
 hipError_t delta_half_fwd(const DeltaArgs &a, hipStream_t s) {
   const DeltaLayout l = delta_half_layout(a);
   const Ws w = carve(l, a.ws);
-  const hipError_t e = l.chunks > 0 ? prep<false>(a, l, w, s) : hipSuccess;
-  return e != hipSuccess ? e : scan(a, l, w, s);
+  return scan(a, l, w, s);
 }
 hipError_t delta_half_bwd(const DeltaArgs &a, hipStream_t s) {
   const DeltaLayout l = delta_half_layout(a);
@@ -1314,7 +1367,7 @@ hipError_t delta_half_bwd(const DeltaArgs &a, hipStream_t s) {
     f.HT = nullptr;
     if ((e = delta_half_fwd(f, s)) != hipSuccess) return e;
   }
-  if (l.chunks > 0 && (e = prep<true>(a, l, w, s)) != hipSuccess) return e;
+  if (l.chunks > 0 && (e = prep<true>(a, l, 0, l.chunks, w, s)) != hipSuccess) return e;
   e = a.K == 32 ? bwd_k<32>(a, l, w, s) : a.K == 64 ? bwd_k<64>(a, l, w, s) : bwd_k<128>(a, l, w, s);
   if (e != hipSuccess || l.chunks == 0 || a.N == a.Nqk) return e;
   const size_t vecs = (size_t)a.B * a.T * a.Nqk * (a.K / 4);

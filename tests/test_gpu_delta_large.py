@@ -117,6 +117,25 @@ def test_gradients_of_segments_in_place(torch, io, K, V):
     small.check(dict(got, HT=state, dH0=grad), {n: want[n] for n in list(got) + ["HT", "dH0"]}, (io, K, V))
 
 
+# 64 states in 128 workgroups: more than 16 chunks go in several launches
+@pytest.mark.parametrize("K", [32, 64, 128])
+@pytest.mark.parametrize("T", [1024, 1025, 2200])
+def test_few_long_sequences(torch, K, T):
+    print("case", K, T, flush=True)
+    s = dr.rule_inputs(46, 2, T, 32, K, 32, Nqk=16, io="bf16")
+    want = dr.rule(s)
+    a, b = small.run(s, "bf16"), small.run(s, "bf16", use_ckpt=False)
+    small.check(a, want, (K, T))
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    c = small.run(s, "bf16", backward=False)
+    assert torch.equal(a["y"], c["y"]) and torch.equal(a["HT"], c["HT"])
+    d = small.device(s, "bf16")  # the state in place
+    p = mb.Delta(2, T, 32, K, 32, "bf16", Nqk=16, backward=False)
+    p.HT = d["H0"]
+    y, HT = p.fwd(*(d[n] for n in ("q", "k", "v", "g", "beta", "H0")))
+    assert torch.equal(a["y"], y) and torch.equal(a["HT"], HT)
+
+
 def test_norm_and_window_captured(torch):
     """Replayed three times on other inputs, with eager work in between; the window is carried in place."""
     B, T, G, L, io = 2, 65, 6, 64, "bf16"
