@@ -406,7 +406,8 @@ struct Part {
   float *HT;
 };
 // Y: y is wanted;  CKPT: the chunks' states and U are.  8 x 4096 steps, 16 heads of 64 x 64: 163 us, 2.5 a chunk on
-// 256 workgroups (3.5 TB/s); 65 536 steps, 32 of 64 x 64 without checkpoints: 1.33 a chunk on 128 of them.
+// 256 workgroups (3.5 TB/s); 65 536 steps, 32 of 64 x 64 without checkpoints: 1.4 a chunk on 128 of them,
+// T and P of later chunks beside it.
 template <int K, int VB, bool Y, bool CKPT>
 __global__ void __launch_bounds__(256, 2)
     delta_half_fwd_kernel(DeltaArgs a, int chunks, Part p, float *gates, half_t *mats, half_t *__restrict__ states,
