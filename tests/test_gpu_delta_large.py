@@ -173,3 +173,64 @@ def test_norm_and_window_captured(torch):
         assert torch.equal(t["win"], win)
         for n in want:
             assert torch.equal(out[n], want[n]), n
+
+
+@pytest.mark.parametrize("io,B,T,N,Nqk,K,V", [("bf16", 2, 1100, 32, 16, 32, 32), ("bf16", 3, 130, 4, 2, 64, 256), ("bf16", 2, 65, 3, 3, 128, 64),
+                                              ("f32", 2, 70, 4, 2, 64, 32), ("bf16", 2, 33, 2, 1, 16, 16)])
+@pytest.mark.parametrize("use_ckpt", [True, False])
+def test_room_of_exactly_the_queried_size(torch, io, B, T, N, Nqk, K, V, use_ckpt):
+    """Checkpoints and workspace end where the queries say: what lies in front of and behind them stays as it was."""
+    print("case", io, B, T, N, Nqk, K, V, use_ckpt, flush=True)
+    s = dr.rule_inputs(47, B, T, N, K, V, Nqk=Nqk, io=io)
+    d, want = small.device(s, io), small.run(s, io, use_ckpt=use_ckpt)
+    desc = mb.make_desc(B=B, T=T, N=N, K=K, V=V, io=mb.M2RNN_BF16 if io == "bf16" else mb.M2RNN_F32, Nqk=Nqk)
+    st, guard = torch.cuda.current_stream().cuda_stream, 4096
+
+    def room(n):
+        whole = torch.full((n + 2 * guard,), 0xA5, dtype=torch.uint8, device="cuda")
+        return whole, whole[guard:guard + n]
+
+    kept = [room(mb.m2rnn_delta_ckpt_bytes(desc)), room(mb.m2rnn_delta_workspace_bytes(desc, 0)),
+            room(mb.m2rnn_delta_workspace_bytes(desc, 1 if use_ckpt else 2))]
+    got = {n: torch.full_like(x, float("nan")) for n, x in want.items()}
+    args = [d[n] for n in ("q", "k", "v", "g", "beta", "H0")]
+    mb.m2rnn_delta_fwd(desc, *args, got["y"], got["HT"], kept[0][1] if use_ckpt else None, kept[1][1], stream=st)
+    mb.m2rnn_delta_bwd(desc, *args, kept[0][1] if use_ckpt else None, d["dy"], d["dHT"], *(got[n] for n in dr.RULE_NAMES),
+                       kept[2][1], stream=st)
+    torch.cuda.synchronize()
+    for whole, _ in kept:
+        assert (whole[:guard] == 0xA5).all() and (whole[-guard:] == 0xA5).all()
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+
+
+def test_long_parts_captured(torch):
+    """A forward of several launches, captured, replayed on other inputs with eager work in between."""
+    T, N, K, V = 2200, 64, 64, 32
+    first = dr.rule_inputs(48, 1, T, N, K, V, io="bf16")
+    d = small.device(first, "bf16")
+    names = ("q", "k", "v", "g", "beta", "H0")
+    p, other = (mb.Delta(1, T, N, K, V, "bf16", backward=False) for _ in range(2))
+    p.fwd(*(d[n] for n in names))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = p.fwd(*(d[n] for n in names))
+    for seed in (49, 50, 51):
+        s = small.device(dr.rule_inputs(seed, 1, T, N, K, V, io="bf16"), "bf16")
+        want = other.fwd(*(s[n] for n in names))
+        for n in names:
+            d[n].copy_(s[n])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, w) for x, w in zip(out, want)), seed
+
+
+@pytest.mark.parametrize("K", [32, 64, 128])
+@pytest.mark.parametrize("V", [32, 64])
+def test_many_states_without_checkpoints(torch, K, V):
+    s = dr.rule_inputs(52, 33, 70, 4, K, V, Nqk=2, io="bf16")
+    y, HT, _ = dr.rule_fwd(*(s[n] for n in ("q", "k", "v", "g", "beta", "H0")))
+    a, b = small.run(s, "bf16"), small.run(s, "bf16", backward=False)
+    small.check(b, {"y": y, "HT": HT}, (K, V))
+    assert torch.equal(a["y"], b["y"]) and torch.equal(a["HT"], b["HT"])
