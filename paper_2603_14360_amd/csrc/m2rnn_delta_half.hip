@@ -61,8 +61,19 @@ struct Pair4 {
   u2_t hi, lo;
 };
 __device__ __forceinline__ Pair4 split4(f4_t x) {
-  const u2_t a = split2_hi_lo(x[0], x[1]), b = split2_hi_lo(x[2], x[3]);
-  return Pair4{u2_t{a.x, b.x}, u2_t{a.y, b.y}};
+  Pair4 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    // (hi to nearest: on its own it is the operand of what becomes bf16, y among it, and cut towards zero it would
+    // make all of that smaller by 2^-12)
+    const uint32_t hi = pack2_h(x[2 * i], x[2 * i + 1]);
+    float l0, l1;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(l0) : "v"(hi), "v"(x[2 * i]));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(l1) : "v"(hi), "v"(x[2 * i + 1]));
+    r.hi[i] = hi;
+    r.lo[i] = pack2_h(l0, l1);
+  }
+  return r;
 }
 __device__ __forceinline__ h8_t ld8(const half_t *p) { return *(const h8_t *)p; }
 __device__ __forceinline__ h8_t tr8(const half_t *p0, const half_t *p1) {
