@@ -55,6 +55,7 @@ struct DeltaLayout {
   size_t carry;   // the states between the launches of a forward (0: there is one)
   size_t states;  // one state per chunk
   size_t rows;    // U or Z of every step
+  size_t exps;    // with the checkpoints: the powers of two of states and U (0: none)
   size_t scales;  // powers of two of the gradients (0: none)
   size_t heads;   // dq or dk of every head in fp32 (0 where no heads share q, k)
 };

@@ -35,7 +35,7 @@ DeltaLayout layout(const DeltaArgs &a) { return half(a) ? delta_half_layout(a) :
 hipError_t run_fwd(const DeltaArgs &a, hipStream_t s) { return half(a) ? delta_half_fwd(a, s) : delta_f32_fwd(a, s); }
 hipError_t run_bwd(const DeltaArgs &a, hipStream_t s) { return half(a) ? delta_half_bwd(a, s) : delta_f32_bwd(a, s); }
 
-size_t ckpt_bytes(const DeltaLayout &l) { return l.states + l.rows + (l.kept ? l.gates + l.mats : 0); }
+size_t ckpt_bytes(const DeltaLayout &l) { return l.states + l.rows + l.exps + (l.kept ? l.gates + l.mats : 0); }
 size_t ws_bytes(const DeltaLayout &l, int bwd) {
   const size_t fwd = l.gates + l.mats + l.carry;
   return bwd ? fwd + l.states + l.rows + l.scales + 2 * l.heads + (bwd >= 2 ? ckpt_bytes(l) : 0) : fwd;

@@ -10,7 +10,8 @@
 // Operands.  q, k, v, dy are bf16 and exact as fp16 (magnitudes from 2^-17 to 2^15).  Everything that reaches a
 // state enters its product as an fp16 pair hi + lo of 22 bits, so that states and their gradients, which are
 // fp32, are as good as that; what only reaches a bf16 result is one fp16 value of 11 bits.  T is formed in fp32.
-// Gradients may have any magnitude: a chunk's are brought near one by a power of two first.
+// The rule is linear in v and H, and its gradients in dy and dH: a chunk's state, its R and U, and its gradients are
+// brought near one by powers of two first, per workgroup, and may have any magnitude.
 //
 // Layout.  Products are D = A B^T: a lane gives eight elements of row (lane % 16) of a factor, and holds rows
 // 4 (lane / 16) .. + 3 of column lane % 16 of D.  Which eight of the 32 that are contracted is free, as long as both
@@ -28,7 +29,9 @@ namespace {
 
 constexpr int C = 64;
 constexpr int LC = C + 8;       // halfs per row of an LDS array with a chunk's steps side by side
-constexpr int kGates = 5 * C;   // floats per chunk: e^G, e^{G_C - G}, G / ln 2 as hi, lo, beta
+// Floats per chunk: e^G, e^{G_C - G}, G / ln 2 as hi, lo, beta, and as ints at kTops the exponents (floor log2) of the
+// largest |k| and |beta|
+constexpr int kTops = 5 * C, kGates = kTops + 16;
 // (Backward: e^G over om = 2^floor(G_0 / ln 2).  e^G goes into fp16 operands there, all of it can be as small as
 // the first step's gate, and the gradient of the state in front is then as small: om is put back in fp32.)
 __device__ __forceinline__ float gate_unit(float hi0) { return exp2_(floorf(hi0)); }
@@ -76,6 +79,46 @@ __device__ __forceinline__ Pair4 split4(f4_t x) {
   return r;
 }
 __device__ __forceinline__ h8_t ld8(const half_t *p) { return *(const h8_t *)p; }
+
+// The largest finite magnitude of a wave's values, of which `each` calls back with all that a lane has.  Infinities
+// and NaN do not count: they are no measure for the values beside them.  (fmaxf passes over a NaN; an infinity, which
+// is rare, costs a second pass without it.)
+template <typename F>
+__device__ __forceinline__ float wave_top(F each) {
+  float top = 0.f;
+  each([&](float x) { top = fmaxf(top, fabsf(x)); });
+  top = group_max_nonneg<64>(top);
+  if (__builtin_bit_cast(int, top) == 0x7F800000) {
+    top = 0.f;
+    each([&](float x) { top = fabsf(x) < __builtin_inff() ? fmaxf(top, fabsf(x)) : top; });
+    top = group_max_nonneg<64>(top);
+  }
+  return top;
+}
+// the exponent of the largest of four waves' tops, the same in all lanes and so in a scalar register; such that 2^e and
+// 2^-e are both normal numbers
+__device__ __forceinline__ int exponent_in_range(int e) { return min(max(e, -126), 126); }
+__device__ __forceinline__ int exponent_of(u4_t tops) {
+  const uint32_t top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+  return exponent_in_range(ilog2f(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(top))));
+}
+__device__ __forceinline__ int exponent_of(f4_t tops) { return exponent_of(__builtin_bit_cast(u4_t, tops)); }
+// eight bf16 magnitudes into the largest finite ones so far, two at a time, as bits + 0x80: what is not finite is
+// negative then.  Start from kNoBf16Top.
+typedef short s2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short us2_t __attribute__((ext_vector_type(2)));
+constexpr short kNoBf16Top = 0x80;
+__device__ __forceinline__ s2_t bf16_top(u4_t w, s2_t top) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const us2_t x = __builtin_bit_cast(us2_t, w[i] & 0x7FFF7FFFu) + us2_t{0x80, 0x80};
+    top = __builtin_elementwise_max(top, __builtin_bit_cast(s2_t, x));
+  }
+  return top;
+}
+__device__ __forceinline__ float bf16_top_value(s2_t top) {
+  return __builtin_bit_cast(float, (uint32_t)(max((int)top.x, (int)top.y) - 0x80) << 16);
+}
 __device__ __forceinline__ h8_t tr8(const half_t *p0, const half_t *p1) {
   const h4_t a = lds_ld_tr((const lchar *)p0, 0), b = lds_ld_tr((const lchar *)p1, 0);
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -117,7 +160,7 @@ __device__ __forceinline__ f4_t mma_f32(f4_t a, f4_t b, f4_t c) {
 // What bounds it is latency: all loads are issued at once, and 24 KB of LDS leave room for six workgroups per CU.
 // 8 x 4096 steps, 16 heads of 64 x 64: 65 us forward, 98 backward (3.5 TB/s, mostly of T and P).
 struct PrepLds {
-  float As[C][C + 4], Xt[C / 2][C / 2 + 4], hi[C], lo[C], be[C];
+  float As[C][C + 4], Xt[C / 2][C / 2 + 4], hi[C], lo[C], be[C], tops[4];
 };
 template <int K, bool BWD>
 __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int unit, int ch, float *gates, half_t *mats,
@@ -163,8 +206,16 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int u
     gt[2 * C + lane] = G.hi;
     gt[3 * C + lane] = G.lo;
     gt[4 * C + lane] = beta;
+    const float top = wave_top([&](auto put) { put(beta); });
+    if (lane == 0) ((int *)gt)[kTops + 1] = exponent_in_range(ilog2f(top));
   }
+  s2_t ktop = {kNoBf16Top, kNoBf16Top};
+#pragma unroll
+  for (int e = 0; e < KB; ++e) ktop = bf16_top(kw[e], ktop);
+  const float kmax = group_max_nonneg<64>(bf16_top_value(ktop));
+  if (lane == 0) lds.tops[wv] = kmax;
   __syncthreads();
+  if (threadIdx.x == 0) ((int *)(gates + slot * kGates))[kTops] = exponent_of(*(const f4_t *)lds.tops);
   u2_t ph[4], pl[4];  // P's four columns (rows, transposed) per tile: an operand's halves as they are
 #pragma unroll
   for (int o = 0; o < 4; ++o) ph[o] = pl[o] = u2_t{0u, 0u};
@@ -380,12 +431,16 @@ struct Gates {
   float *at;  // 64 of the wave
   static __device__ __forceinline__ uint32_t offset(int wv) {
     const int lane = threadIdx.x & 63, i = lane & 15;
-    return 4 * (lane < 16 ? 16 * wv + i : lane < 32 ? C + 16 * wv + i : lane < 48 ? 4 * C + 16 * wv + i : i == 0 ? C - 1 : 2 * C);
+    return 4 * (lane < 16 ? 16 * wv + i : lane < 32 ? C + 16 * wv + i : lane < 48 ? 4 * C + 16 * wv + i
+                : i == 0 ? C - 1 : i == 1 ? 2 * C : kTops + (i & 1));
   }
   __device__ __forceinline__ f4_t four(int which) const { return *(const f4_t *)(at + 16 * which + 4 * ((threadIdx.x & 63) >> 4)); }
   __device__ __forceinline__ float one(int which) const { return at[16 * which + (threadIdx.x & 15)]; }
   __device__ __forceinline__ float last() const { return at[48]; }    // e^G of the chunk's last step
   __device__ __forceinline__ float first() const { return at[49]; }   // hi of its first
+  __device__ __forceinline__ int top(int i) const { return __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, at[50 + i])); }
+  __device__ __forceinline__ int k_top() const { return top(0); }
+  __device__ __forceinline__ int beta_top() const { return top(1); }
 };
 // A wave's 16 steps of VB columns, eight a lane as loaded, through LDS to four steps of one column per lane and
 // column tile, as in D[step][column]
@@ -406,7 +461,55 @@ struct Turn {
 };
 
 template <int K, int VB>
-constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4; }
+constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 24 * 4; }
+
+// The largest |H| (upper 16 bits, cut to them as bf16) and |v| of a workgroup, infinities among them, in two halves of
+// a word: a word for every 16 lanes to LDS, and from there.
+template <typename F, int M, int N>
+__device__ __forceinline__ void all_of(const f4_t (&x)[M][N], F put) {
+#pragma unroll
+  for (int i = 0; i < M * N * 4; ++i) put(x[i / (4 * N)][i / 4 % N][i % 4]);
+}
+template <typename F, int M>
+__device__ __forceinline__ void all_of(const f4_t (&x)[M], F put) {
+#pragma unroll
+  for (int i = 0; i < M * 4; ++i) put(x[i / 4][i % 4]);
+}
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2_t, a), __builtin_bit_cast(us2_t, b)));
+}
+template <int M, int N, int VT>
+__device__ __forceinline__ void top_of_rows(uint32_t *red, const f4_t (&H)[M][N], const f4_t (&v)[VT], int wv) {
+  float th = 0.f, tw = 0.f;
+  all_of(H, [&](float x) { th = fmaxf(th, fabsf(x)); });
+  all_of(v, [&](float x) { tw = fmaxf(tw, fabsf(x)); });
+  uint32_t t = (__builtin_bit_cast(uint32_t, th) & 0xFFFF0000u) | (__builtin_bit_cast(uint32_t, tw) >> 16);
+  t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0xB1, 0xF, 0xF, false));   // quad_perm [1,0,3,2]
+  t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
+  t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x141, 0xF, 0xF, false));  // row_half_mirror
+  t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x140, 0xF, 0xF, false));  // row_mirror
+  if ((threadIdx.x & 15) == 0) red[4 * wv + ((threadIdx.x & 63) >> 4)] = t;
+}
+__device__ __forceinline__ uint32_t top_of_all(const uint32_t *red) {
+  u4_t m = *(const u4_t *)red;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    const u4_t x = *(const u4_t *)(red + 4 * i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = max_halves(m[j], x[j]);
+  }
+  return __builtin_amdgcn_readfirstlane(max_halves(max_halves(m[0], m[1]), max_halves(m[2], m[3])));
+}
+// the exponent of the lower 16 bits of x as bf16
+__device__ __forceinline__ int top_exponent(uint32_t x) { return max((int)(x >> 7 & 255u) - 127, -126); }
+__device__ __forceinline__ bool not_finite(uint32_t tops) {
+  return (tops & 0x7F800000u) == 0x7F800000u || (tops & 0x7F80u) == 0x7F80u;
+}
+
+// Forward.  The state lies in registers over 2^eh, which stays while its largest entry is between 2^-2 and 2^13 of
+// that; R and U are over 2^er, from the chunk's largest |H|, |v|, |k| and |beta|.  The largest |H| is known to all waves
+// only behind the barrier that hands the state over: a state that has left its range is then handed over again, scaled anew
+// (which a sequence does a few times at its start).
 
 // What a launch of the forward does: the chunks c0 .. c1 - 1 of all states, from H0 to HT, in its first `scans`
 // workgroups, and T and P of the chunks c1 .. c2 - 1, which the next launch reads, in the others.
@@ -422,12 +525,13 @@ struct Part {
 template <int K, int VB, bool Y, bool CKPT>
 __global__ void __launch_bounds__(256, 2)
     delta_half_fwd_kernel(DeltaArgs a, int chunks, Part p, float *gates, half_t *mats, half_t *__restrict__ states,
-                          half_t *__restrict__ rows_u) {
+                          half_t *__restrict__ rows_u, int *__restrict__ exps) {
   using S = Scan<K, VB>;
   constexpr int KB = S::KB, KT = S::KT, VT = S::VT, KTW = S::KTW, VTW = S::VTW, LK = S::LK;
   extern __shared__ __align__(16) char lds[];
   half_t *ks = (half_t *)lds, *Ht = ks + C * LK, *Hl = Ht + VB * LK, *Rt = Hl + VB * LK, *Rl = Rt + VB * LC;
   half_t *Ut = Rl + VB * LC, *Wt = Ut + VB * LC, *Wl = Wt + VB * LC, *turn = Wl + VB * LC;
+  uint32_t *red = (uint32_t *)(turn + 4 * Turn<VB>::HALFS) + 4 * 64;
   int unit, part;
   if (blockIdx.x >= p.scans) {
     const int i = blockIdx.x - p.scans, n = p.c2 - p.c1;
@@ -457,6 +561,11 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         H[i][j][x] = p.H0 ? p.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
+  // (here, and not at the head of the loop, which would then wait for everything in each of its rounds)
+#pragma unroll
+  for (int i = 0; i < KTW; ++i)
+#pragma unroll
+    for (int j = 0; j < VTW; ++j) settle(H[i][j]);
   // The next chunk's, in the order of their use: k, v and gates in its first product, T in its second, q and P last.
   // Each load is issued behind the last use of its registers and so has most of a chunk to arrive.
   u4_t nk[KB], nq[KB], nv;
@@ -484,6 +593,7 @@ __global__ void __launch_bounds__(256, 2)
   h8_t kf[KB];
   f4_t vf[VT], ge, gl, be;
   float g1, gc;
+  int ek, eb, eh = 0;
   auto take1 = [&]() {
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
@@ -495,6 +605,7 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
     for (int t = 0; t < VT; ++t) vf[t] = tv.get(t);
     ge = gs.four(0); gl = gs.four(1); be = gs.four(2); g1 = gs.one(0); gc = gs.last();
+    ek = gs.k_top(); eb = gs.beta_top();
   };
   auto put_state = [&]() {
     if (S::on(wv))
@@ -502,25 +613,19 @@ __global__ void __launch_bounds__(256, 2)
       for (int i = 0; i < KTW; ++i)
 #pragma unroll
         for (int j = 0; j < VTW; ++j) {
-          const Pair4 s = split4(H[i][j]);
+          const Pair4 x = split4(H[i][j]);
           const int o = (16 * S::vt(wv, j) + d) * LK + 16 * S::kt(wv, i) + 4 * g4;
-          *(u2_t *)&Ht[o] = s.hi;
-          *(u2_t *)&Hl[o] = s.lo;
+          *(u2_t *)&Ht[o] = x.hi;
+          *(u2_t *)&Hl[o] = x.lo;
         }
   };
-  put_state();
   if (p.c0 < p.c1) {
     fetch1(p.c0);
     fetch2(p.c0);
     if (Y) fetch3(p.c0);
     take1();
   }
-  const int w = place(wv);
-  for (int ch = p.c0; ch < p.c1; ++ch) {
-    const int next = min(ch + 1, p.c1 - 1);
-    lds_barrier();  // the state is there, and k of the chunk before has been read
-    // R = beta (v - e^G K H): D[step][column]
-    h8_t hh[VT][KB], hl[VT][KB];
+  auto get_state = [&](h8_t(&hh)[VT][KB], h8_t(&hl)[VT][KB]) {
 #pragma unroll
     for (int i = 0; i < KB; ++i)
 #pragma unroll
@@ -529,22 +634,79 @@ __global__ void __launch_bounds__(256, 2)
         hh[t][i] = ld8(Ht + o);
         hl[t][i] = ld8(Hl + o);
       }
+  };
+  // R is no larger than sqrt(K) 2^er, and U not by much more while the rule does not expand.  The state counts as no
+  // smaller than 2^-24 of that, of which nothing would be left beside it.
+  auto scale_for = [&](int et, int ev, int &er) {
+    er = exponent_in_range(eb + max(ev, ek + et));
+    return max(exponent_in_range(et), er - 24);
+  };
+  // The exponents of the largest finite |H| and |v|
+  auto measure = [&](int &et, int &ev) {
+    const float th = wave_top([&](auto put) { all_of(H, put); }), tw = wave_top([&](auto put) { all_of(vf, put); });
+    if (lane == 0) {
+      red[16 + wv] = __builtin_bit_cast(uint32_t, th);
+      red[20 + wv] = __builtin_bit_cast(uint32_t, tw);
+    }
+    lds_barrier();
+    et = eh + exponent_of(*(const u4_t *)(red + 16));
+    ev = exponent_of(*(const u4_t *)(red + 20));
+  };
+  auto rescale = [&](int to) {
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) H[i][j][x] = __builtin_amdgcn_ldexpf(H[i][j][x], eh - to);
+    eh = to;
+  };
+  if (p.c0 < p.c1) {
+    int et, ev, er;
+    measure(et, ev);
+    rescale(scale_for(et, ev, er));
+  }
+  const int w = place(wv);
+  for (int ch = p.c0; ch < p.c1; ++ch) {
+    const int next = min(ch + 1, p.c1 - 1);
+    put_state();
 #pragma unroll
     for (int i = 0; i < KB; ++i) *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
-    fetch1(next);
+    top_of_rows(red, H, vf, wv);
+    lds_barrier();  // the state is there, and k of the chunk before has been read
+    // R = beta (v - e^G K H): D[step][column]
+    const uint32_t tops = top_of_all(red);
+    h8_t hh[VT][KB], hl[VT][KB];
     f4_t x[VT], xl[VT];
+    auto keys_with_state = [&]() {
 #pragma unroll
-    for (int t = 0; t < VT; ++t) x[t] = xl[t] = zero;
+      for (int t = 0; t < VT; ++t) x[t] = xl[t] = zero;
 #pragma unroll
-    for (int i = 0; i < KB; ++i)
+      for (int i = 0; i < KB; ++i)
 #pragma unroll
-      for (int t = 0; t < VT; ++t) {
-        x[t] = mfma_k32(kf[i], hh[t][i], x[t]);
-        xl[t] = mfma_k32(kf[i], hl[t][i], xl[t]);
-      }
+        for (int t = 0; t < VT; ++t) {
+          x[t] = mfma_k32(kf[i], hh[t][i], x[t]);
+          xl[t] = mfma_k32(kf[i], hl[t][i], xl[t]);
+        }
+    };
+    get_state(hh, hl);
+    fetch1(next);
+    keys_with_state();
+    int et = eh + top_exponent(tops >> 16), ev = top_exponent(tops), er;
+    int want = scale_for(et, ev, er);
+    if (not_finite(tops) || want < eh - 2 || want > eh + 13) {  // (the same in all waves)
+      measure(et, ev);
+      want = scale_for(et, ev, er);
+      rescale(want);
+      put_state();
+      lds_barrier();
+      get_state(hh, hl);
+      keys_with_state();
+    }
+    const f4_t gh = pow2i(eh) * ge, br = pow2i(-er) * be;
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
-      const Pair4 s = split4(be * (vf[t] - ge * (x[t] + xl[t])));
+      const Pair4 s = split4(br * (vf[t] - gh * (x[t] + xl[t])));
       *(u2_t *)&Rt[(16 * t + d) * LC + w] = s.hi;
       *(u2_t *)&Rl[(16 * t + d) * LC + w] = s.lo;
     }
@@ -594,6 +756,7 @@ __global__ void __launch_bounds__(256, 2)
     lds_barrier();
     // H = e^{G_C} H + K^T W: D[row][column];  y = e^G (Q H)^T + (P U)^T
     h8_t wh[VTW][2], wl[VTW][2], uf[VT][2], us;
+    const float gy = pow2i(eh) * g1, ru = pow2i(er), rus = pow2i(er - eh);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -610,24 +773,23 @@ __global__ void __launch_bounds__(256, 2)
         for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf, y[t]);
       }
     }
-#pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) H[i][j] *= gc;
+    f4_t kw[KTW][VTW];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < KTW; ++i)
 #pragma unroll
         for (int j = 0; j < VTW; ++j) {
-          H[i][j] = mfma_k32(kT[i][kb], wl[j][kb], H[i][j]);
-          H[i][j] = mfma_k32(kT[i][kb], wh[j][kb], H[i][j]);
+          kw[i][j] = mfma_k32(kT[i][kb], wl[j][kb], kb ? kw[i][j] : zero);
+          kw[i][j] = mfma_k32(kT[i][kb], wh[j][kb], kw[i][j]);
         }
 #pragma unroll
     for (int i = 0; i < KTW; ++i)
 #pragma unroll
-      for (int j = 0; j < VTW; ++j) settle(H[i][j]);
-    put_state();
+      for (int j = 0; j < VTW; ++j) {
+        settle(kw[i][j]);
+        H[i][j] = gc * H[i][j] + rus * kw[i][j];
+      }
     if (Y) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -635,14 +797,17 @@ __global__ void __launch_bounds__(256, 2)
         for (int t = 0; t < VT; ++t) uf[t][kb] = ld8(Ut + (16 * t + d) * LC + 32 * kb + 8 * g4);
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
-        y[t] = mfma_k32(uf[t][0], Pf[0], g1 * y[t]);
-        y[t] = mfma_k32(uf[t][1], Pf[1], y[t]);
+        u[t] = mfma_k32(uf[t][0], Pf[0], zero);
+        u[t] = mfma_k32(uf[t][1], Pf[1], u[t]);
       }
       hold();
       fetch3(next);
       hold();
 #pragma unroll
-      for (int t = 0; t < VT; ++t) settle(y[t]);
+      for (int t = 0; t < VT; ++t) {
+        settle(u[t]);
+        y[t] = gy * y[t] + ru * u[t];
+      }
     }
     if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
     take1();
@@ -658,8 +823,12 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
         for (int i = 0; i < KTW; ++i) *(h8_t *)(states + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
       *(h8_t *)(rows_u + at * C * a.V + frag_at<VB>(part, 4, wv)) = us;
+      // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
+      __builtin_amdgcn_raw_buffer_store_b32(lane ? er : eh, __builtin_amdgcn_make_buffer_rsrc(exps + (at * (a.V / VB) + part) * 2,
+                                            0, 8, 0x00027000), 4 * (int)threadIdx.x, 0, 0);
     }
   }
+  rescale(0);
   if (p.HT && S::on(wv))
 #pragma unroll
     for (int i = 0; i < KTW; ++i)
@@ -1005,7 +1174,7 @@ template <int K, int V32>
 __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
     delta_half_grad_kernel(DeltaArgs a, int chunks, int vbs, const float *__restrict__ gates,
                            const half_t *__restrict__ states, const half_t *__restrict__ rows_u,
-                           const half_t *__restrict__ dstates, const half_t *__restrict__ rows_z,
+                           const int *__restrict__ exps, const half_t *__restrict__ dstates, const half_t *__restrict__ rows_z,
                            const float *__restrict__ scales, float *__restrict__ dq_heads, float *__restrict__ dk_heads) {
   constexpr int KB = K / 32, KT = K / 16, LK = K + 8;
   constexpr bool ONE = V32 > 2;
@@ -1031,8 +1200,19 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   }
   const half_t *U = rows_u + at * C * a.V + lane * 8, *Z = rows_z + at * C * a.V + (size_t)wv * 512 + lane * 8;
   const half_t *h0 = states + at * K * a.V + lane * 8, *h1 = dstates + at * K * a.V + lane * 8;
-  // the chunk's common power of two: that of the block with the largest gradients
+  // States and U of a block of columns (one of `blocks`) come with a power of two of their own; the chunk's common one is
+  // the largest.  Lanes below 16 have the blocks' factors to it of the states, the next 16 of U.
   const int blocks = a.V / vbs;
+  const bool mine = lane < 32 && (lane & 15) < blocks;
+  const int el = mine ? exps[(at * blocks + (lane & 15)) * 2 + (lane >> 4)] : -1000;
+  const int et = __builtin_bit_cast(int, group_max_nonneg<16>(__builtin_bit_cast(float, el + 1000))) - 1000;
+  const int eh = __builtin_amdgcn_readlane(et, 0), eu = __builtin_amdgcn_readlane(et, 16);
+  const int fl = __builtin_bit_cast(unsigned short, (half_t)pow2i(el - et));
+  auto own_factor = [&](int kind, int vb) {
+    const half_t f = __builtin_bit_cast(half_t, (unsigned short)__shfl(fl, 16 * kind + (vbs == 32 ? vb : 2 * vb + (g4 >> 1)), 64));
+    return h8_t{f, f, f, f, f, f, f, f};
+  };
+  // the gradients' common power of two: that of the block with the largest
   const float *sb = scales + at * blocks;
   float sc = sb[0];
   for (int x = 1; x < blocks; ++x) sc = fminf(sc, sb[x]);
@@ -1047,7 +1227,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
     *(h8_t *)&ks[i * LK + 32 * e + 8 * g4] = bf16_to_h8(kr[e]);
     *(h8_t *)&qs[i * LK + 32 * e + 8 * g4] = bf16_to_h8(qr[e]);
   }
-  for (int x = threadIdx.x; x < kGates; x += 256) {
+  for (int x = threadIdx.x; x < kTops; x += 256) {
     const float g = gates[at * kGates + x];
     ge[x] = g;
     if (x >= 4 * C) bh[x - 4 * C] = (half_t)g;
@@ -1060,17 +1240,18 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   for (int x = 0; x < KT; ++x) dq[x] = as[x] = kept[x] = zero;
   float zv = 0.f, hd = 0.f;
   auto with_states = [&](int vb, h8_t f8, h8_t y, h8_t z, h8_t u) {
-    const h8_t uf = u * f8;  // (for dH, whose power of two it is)
+    const h8_t uf = u * (f8 * own_factor(1, vb));  // (f8: for dH, whose power of two it is)
+    const h8_t fh = own_factor(0, vb), yh = y * fh, zh = z * fh;
     float hb = 0.f;
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
       const h8_t x0 = ld8(h0 + (vb * KT + x) * 512), x1 = ld8(h1 + (vb * KT + x) * 512);
-      dq[x] = mfma_k32(x0, y, dq[x]);
-      as[x] = mfma_k32(x0, z, as[x]);
+      dq[x] = mfma_k32(x0, yh, dq[x]);
+      as[x] = mfma_k32(x0, zh, as[x]);
       kept[x] = mfma_k32(x1, uf, kept[x]);
       if ((x & 3) == wv) hb = dot8(x0, x1, hb);
     }
-    hd = fmaf((float)f8[0], hb, hd);
+    hd = fmaf((float)f8[0] * (float)fh[0], hb, hd);
   };
 #pragma unroll
   for (int vb = 0; vb < (ONE ? 1 : V32); ++vb)
@@ -1081,13 +1262,14 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
       bf16x8_to_f32(buf_ld(rv, ov + 64 * vo), vv);
 #pragma unroll
       for (int x = 0; x < 8; ++x) zv = fmaf((float)z[x], vv[x], zv);
+      const h8_t fu = own_factor(1, vo), yu = y * fu, zu = z * fu;
       h8_t u = {};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {  // D[j][i], of which j <= i counts
         if (ONE && j > wv) break;
         u = ld8(U + (vo * 4 + j) * 512);
-        s1[j] = mfma_k32(u, y, s1[j]);
-        s2[j] = mfma_k32(u, z, s2[j]);
+        s1[j] = mfma_k32(u, yu, s1[j]);
+        s2[j] = mfma_k32(u, zu, s2[j]);
       }
       if (ONE) with_states(vo, f8, y, z, u);  // (the last u is my own)
     }
@@ -1097,8 +1279,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
     settle(s2[j]);
   }
   __syncthreads();
-  // S1, S2 masked; their largest entry, so that they can be fp16 whatever U is
-  float top = 0.f;
+  // S1, S2 masked; their largest entries, so that they can be fp16 whatever U is
   const float ghi = ge[2 * C + i], glo = ge[3 * C + i];
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt)
@@ -1110,23 +1291,35 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
         const float e = exp2_((ghi - h[x]) + (glo - l[x]));
         s1[jt][x] = j <= i ? e * s1[jt][x] : 0.f;
         s2[jt][x] = j < i ? -e * s2[jt][x] : 0.f;
-        top = fmaxf(top, fmaxf(fabsf(s1[jt][x]), fabsf(s2[jt][x])));
       }
     }
-  top = group_max_nonneg<64>(top);
+  const float top1 = wave_top([&](auto put) {
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) put(s1[jt][x]);
+  });
+  const float top2 = wave_top([&](auto put) {
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) put(s2[jt][x]);
+  });
   zv += __shfl_xor(zv, 16, 64);
   zv += __shfl_xor(zv, 32, 64);
-  if (lane == 0) red[wv * 4] = top;
+  if (lane == 0) {
+    red[wv] = top1;
+    red[4 + wv] = top2;
+  }
   __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[4]), fmaxf(red[8], red[12]));
-  const int ex = min(max(ilog2f(top), -100), 100);
-  const float ss = pow2i(-ex), sinv = pow2i(ex), bt = ge[4 * C + i], gt = ge[C + i];
+  const int x1 = exponent_of(*(const f4_t *)red), x2 = exponent_of(*(const f4_t *)(red + 4));
+  const float ss1 = pow2i(-x1), ss2 = pow2i(-x2), bt = ge[4 * C + i], gt = ge[C + i];
   const float om = gate_unit(ge[2 * C]), gm = om * ge[i];
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt) {  // (the last tile of an even wave's pair is zero)
     const int o = i * LC + 16 * jt + 4 * g4;
-    *(u2_t *)&S1[o] = pack4_h(ss * s1[jt]);
-    *(u2_t *)&S2[o] = pack4_h(ss * s2[jt]);
+    *(u2_t *)&S1[o] = pack4_h(ss1 * s1[jt]);
+    *(u2_t *)&S2[o] = pack4_h(ss2 * s2[jt]);
   }
 
   if (!ONE)
@@ -1143,10 +1336,14 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   }
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) hd += __shfl_xor(hd, m, 64);
-  if (lane == 0) red[wv * 4 + 1] = hd;
+  if (lane == 0) red[8 + wv] = hd;
   __syncthreads();
   const bool heads = a.N != a.Nqk;
-  const float inv = 1.f / sc;
+  // every product with the powers of two that its factors came without
+  const int es = -ilog2f(sc), eY = es, eZ = es, eD = es;
+  const float inv = pow2i(eZ);
+  const float cq = gm * pow2i(eh + eY), ca = -gm * pow2i(eh + eZ), ck = gt * pow2i(eu + eD);
+  const float c1 = pow2i(x1 + eu + eY), c2 = pow2i(x2 + eu + eZ);
   float dG = 0.f, kb1 = 0.f, tail = 0.f;
   h8_t row1[2], row2[2], col1[2], colb[2];
 #pragma unroll
@@ -1159,36 +1356,35 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const f4_t kd = kept[kt];
-    f4_t x = (ss * gm) * dq[kt], y = (-ss * gm) * as[kt], w = (ss * gt) * kd;
+    f4_t x = zero, y = zero, w = zero, wb = zero;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       const h8_t kT = ld8_tr(ks, LK, 32 * kb, 16 * kt), qT = ld8_tr(qs, LK, 32 * kb, 16 * kt);
       x = mfma_k32(kT, row1[kb], x);
       y = mfma_k32(kT, row2[kb], y);
       w = mfma_k32(qT, col1[kb], w);
-      w = mfma_k32(kT, colb[kb], w);
+      wb = mfma_k32(kT, colb[kb], wb);
     }
     settle(x);
     settle(y);
     settle(w);
+    settle(wb);
     const h4_t qv = *(const h4_t *)&qs[i * LK + 16 * kt + 4 * g4], kv = *(const h4_t *)&ks[i * LK + 16 * kt + 4 * g4];
     f4_t o;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float qx = (float)qv[r], kx = (float)kv[r];
-      x[r] *= sinv;
-      y[r] *= sinv;
-      w[r] *= sinv;
+      x[r] = fmaf(c1, x[r], cq * dq[kt][r]);
+      y[r] = fmaf(c2, y[r], ca * as[kt][r]);
+      w[r] = fmaf(c1, w[r], fmaf(c2, wb[r], ck * kd[r]));
       o[r] = fmaf(bt, y[r], w[r]);
       dG = fmaf(qx, x[r], dG);
       dG = fmaf(kx, fmaf(bt, y[r], -w[r]), dG);
       kb1 = fmaf(kx, y[r], kb1);
-      tail = fmaf(gt * kx, kd[r], tail);
+      tail = fmaf(ck * kx, kd[r], tail);
     }
     if (own < a.T) {
       const size_t m = ((size_t)b * a.T + own) * (heads ? a.N : a.Nqk) * K + (size_t)(heads ? n : nq) * K + 16 * kt + 4 * g4;
-      x *= inv;
-      o *= inv;
       if (heads) {
         *(f4_t *)&dq_heads[m] = x;
         *(f4_t *)&dk_heads[m] = o;
@@ -1204,22 +1400,22 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   kb1 += __shfl_xor(kb1, 32, 64);
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) tail += __shfl_xor(tail, m, 64);
-  if (lane == 0) red[wv * 4 + 2] = tail;
+  if (lane == 0) red[12 + wv] = tail;
   if (g4 == 0) red[16 + i] = dG;
   if (g4 == 0 && own < a.T)
-    ((__hip_bfloat16 *)a.dbeta)[((size_t)b * a.T + own) * a.N + n] = __float2bfloat16(inv * (zv + kb1));
+    ((__hip_bfloat16 *)a.dbeta)[((size_t)b * a.T + own) * a.N + n] = __float2bfloat16(inv * zv + kb1);
   __syncthreads();
   if (wv == 0) {  // sums over the steps behind, in 64 bits; <H_C, dH> at the last one
     double s = (double)red[16 + lane];
     if (lane == C - 1)
-      for (int w = 0; w < 4; ++w) s += (double)(om * ge[C - 1]) * red[4 * w + 1] + red[4 * w + 2];
+      for (int w = 0; w < 4; ++w) s += (double)(om * ge[C - 1]) * pow2i(eh + eD) * red[8 + w] + red[12 + w];
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
       const double o = __shfl_down(s, m, 64);
       if (lane + m < 64) s += o;
     }
     if (t0 + lane < a.T)
-      ((__hip_bfloat16 *)a.dg)[((size_t)b * a.T + t0 + lane) * a.N + n] = __float2bfloat16((float)(inv * s));
+      ((__hip_bfloat16 *)a.dg)[((size_t)b * a.T + t0 + lane) * a.N + n] = __float2bfloat16((float)s);
   }
 }
 
@@ -1296,7 +1492,8 @@ hipError_t fwd_go(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStre
     p.HT = p.c1 < l.chunks ? w.carry : a.HT;
     hipLaunchKernelGGL((delta_half_fwd_kernel<K, VB, Y, CKPT>), dim3(p.scans + (unsigned)(a.B * a.N) * (unsigned)(p.c2 - p.c1)),
                        dim3(256), lds, s, a, l.chunks, p, w.gates, w.mats, (half_t *)a.ckpt,
-                       a.ckpt ? (half_t *)(a.ckpt + l.states) : nullptr);
+                       a.ckpt ? (half_t *)(a.ckpt + l.states) : nullptr,
+                       a.ckpt ? (int *)(a.ckpt + l.states + l.rows) : nullptr);
     e = hipGetLastError();
     p.c0 = p.c1;
     p.H0 = w.carry;
@@ -1314,8 +1511,8 @@ hipError_t grad_go(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, int vb
   const hipError_t e = set_max_lds_once(delta_half_grad_kernel<K, V32>, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((delta_half_grad_kernel<K, V32>), dim3((unsigned)(a.B * a.N) * (unsigned)l.chunks), dim3(256), lds, s,
-                     a, l.chunks, vb, w.gates, (const half_t *)a.ckpt, (const half_t *)(a.ckpt + l.states), w.dstates,
-                     w.rows_z, w.scales, w.dqh, w.dkh);
+                     a, l.chunks, vb, w.gates, (const half_t *)a.ckpt, (const half_t *)(a.ckpt + l.states),
+                     (const int *)(a.ckpt + l.states + l.rows), w.dstates, w.rows_z, w.scales, w.dqh, w.dkh);
   return hipGetLastError();
 }
 template <int K, int VB>
@@ -1360,6 +1557,7 @@ DeltaLayout delta_half_layout(const DeltaArgs &a) {
   l.carry = part_chunks(a, l.chunks) < l.chunks ? align256((size_t)a.B * a.N * a.K * a.V * sizeof(float)) : 0;
   l.states = align256(n * a.K * a.V * sizeof(half_t));
   l.rows = align256(n * C * a.V * sizeof(half_t));
+  l.exps = align256(n * (a.V / 16) * 2 * sizeof(int));
   l.scales = align256(n * (a.V / 16) * sizeof(float));
   l.heads = a.N != a.Nqk ? align256(steps * a.K * sizeof(float)) : 0;
   return l;

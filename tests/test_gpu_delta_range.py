@@ -1,0 +1,68 @@
+"""GPU: the gated delta rule on magnitudes far from one.
+
+The rule is linear in (v, H0) and its gradients in (dy, dHT), so inputs times a power of two give results times that
+power, to the bit as long as nothing leaves the range of fp32: no tolerance is needed there.  Where inputs of unlike
+size meet, the 64-bit reference at the tolerances of the small tests, of the largest entry that a tensor has met."""
+import numpy as np
+import pytest
+
+import delta_reference as dr
+import gpu_util as gu
+import test_gpu_delta as small
+
+pytestmark = pytest.mark.gpu
+
+# columns of V per workgroup: 16 (few states) and 32
+SIZES = [(2, 130, 3, 64, 64), (2, 70, 2, 128, 32), (3, 65, 2, 32, 256), (33, 66, 4, 64, 32), (17, 70, 2, 128, 128)]
+
+
+def times(s, **exponents):
+    return {n: x if n not in exponents or x is None else x * np.float32(2.0 ** exponents[n]) for n, x in s.items()}
+
+
+def same_but_for(got, base, **exponents):
+    import torch
+    for n, x in base.items():
+        want = x * 2.0 ** exponents.get(n, 0)
+        assert torch.isfinite(got[n]).all() and torch.equal(got[n], want), (n, float((got[n].float() - want.float()).abs().max()))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,N,K,V", SIZES)
+def test_values_and_states_of_any_size(io, B, T, N, K, V):
+    """From 2^-60 to 2^60."""
+    s = dr.rule_inputs(61, B, T, N, K, V, io=io)
+    base = small.run(s, io)
+    for e in (-60, -20, 13, 60):
+        print("case", io, B, T, N, K, V, e, flush=True)
+        got = small.run(times(s, v=e, H0=e), io, use_ckpt=e != 13)
+        same_but_for(got, base, **dict.fromkeys(("y", "HT", "dq", "dk", "dg", "dbeta"), e))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [12, 13, 65, 130])
+@pytest.mark.parametrize("size", [1e4, 1.9e4])
+def test_a_state_along_a_key(io, T, size):
+    """k^T H and with it the updates are sqrt(K) times larger than the state."""
+    s = dr.rule_inputs(62, 2, T, 3, 64, 64, io=io)
+    s["H0"][:] = size
+    s["k"][:, ::5] = 0.125
+    s["g"][:] = s["g"] * np.float32(0.05)
+    want = dr.rule(s)
+    got = small.run(s, io)
+    # (the final state is what is left of one of `size`: its error is one of that)
+    err = np.abs(gu.to_np(got["HT"]) - want.pop("HT")).max()
+    assert err <= small.F32 * size, err
+    # dg = <dH, e^g H> is formed from sums over the chunk's steps of q.(H dy) and -k.(H dv), which cancel.  bf16 io: H in
+    # them is one fp16 value, off by at most 2^-12 of the largest state, each entry on its own; such errors E make
+    # sum_t q_t.(E dy_t) of a standard deviation of at most 2^-12 max|H| sqrt(sum_t |q_t|^2 |dy_t|^2), and k, dv
+    # likewise.  Four of them, beside what every bf16 result may be off.
+    if io == "bf16":
+        dg, norm2 = want.pop("dg"), lambda n: (s.get(n, want.get(n)).astype(np.float64) ** 2).sum(-1)
+        per_step = norm2("q") * norm2("dy") + norm2("k") * norm2("dv")
+        chunk = max(per_step[:, t:t + 64].sum(1).max() for t in range(0, T, 64))
+        lim = small.BF16 * (np.abs(dg) + np.abs(dg).max()) + 4 * 2.0 ** -12 * size * chunk ** 0.5
+        assert (np.abs(gu.to_np(got["dg"]) - dg) <= lim).all(), (T, size)
+    small.check(got, want, (io, T, size))
+    y = gu.to_np(small.run(s, io, backward=False)["y"])
+    assert np.abs(y - want["y"]).max() <= 2 * small.BF16 * np.abs(want["y"]).max()
