@@ -929,18 +929,10 @@ __global__ void __launch_bounds__(256, 2)
   const int w = place(wv);
   for (int ch = chunks - 1; ch >= 0; --ch) {
     const int next = max(ch - 1, 0);
-    float top = 0.f;
-#pragma unroll
-    for (int t = 0; t < VT; ++t)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) top = fmaxf(top, fabsf(yf[t][x]));
-#pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) top = fmaxf(top, fabsf(D[i][j][x]));
-    top = group_max_nonneg<64>(top);
+    const float top = wave_top([&](auto put) {
+      all_of(yf, put);
+      all_of(D, put);
+    });
     if (lane == 0) red[wv] = top;
     lds_barrier();  // (and everything of the chunk before has been read)
     const f4_t tops = *(const f4_t *)red;
@@ -949,8 +941,7 @@ __global__ void __launch_bounds__(256, 2)
       *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
       *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = qf[i];
     }
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const int e = min(max(ilog2f(top), -100), 100);
+    const int e = exponent_of(tops);
     const float s = pow2i(-e), inv = pow2i(e);
     if (S::on(wv))
 #pragma unroll

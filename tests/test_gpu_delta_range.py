@@ -66,3 +66,40 @@ def test_a_state_along_a_key(io, T, size):
     small.check(got, want, (io, T, size))
     y = gu.to_np(small.run(s, io, backward=False)["y"])
     assert np.abs(y - want["y"]).max() <= 2 * small.BF16 * np.abs(want["y"]).max()
+
+
+@pytest.mark.parametrize("bad", [np.inf, np.nan])
+@pytest.mark.parametrize("where", ["dy", "dHT", "v", "H0"])
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_what_is_not_finite_stays_in_its_column(io, where, bad):
+    """One infinity or NaN: y, HT, dv, dH0 of the other columns are as if it had not been there, and so is all of the
+    other heads and batch rows; what it reaches is not finite."""
+    B, T, N, V, t, col = 2, 200, 3, 64, 100, 5
+    s = dr.rule_inputs(63, B, T, N, 64, V, io=io)
+    want = dr.rule(s)
+    if where in ("dy", "v"):
+        s[where][1, t, 2, col] = bad
+    else:
+        s[where][1, 2, 7, col] = bad
+    got = small.run(s, io)
+    top = {n: np.abs(w).max() for n, w in want.items()}
+    for n, w in want.items():
+        g = gu.to_np(got[n])
+        ok = np.ones(w.shape, bool)  # what has to be right
+        if n in ("y", "dv"):
+            ok[1, :, 2, col] = False
+        elif n in ("HT", "dH0"):
+            ok[1, 2, :, col] = False
+        else:
+            ok[1, :, 2] = False
+            if n == "dq" and where in ("dy", "dHT"):  # (dq_t is H_t dy_t: of one step, or of none)
+                ok[1, :, 2] = True
+                ok[1, t, 2] = where == "dHT"
+        lim = small.BF16 * (np.abs(w) + top[n]) if "bfloat16" in str(got[n].dtype) else np.full(w.shape, small.F32 * top[n])
+        assert np.isfinite(g[ok]).all() and (np.abs(g - w)[ok] <= lim[ok]).all(), (n, float(np.nanmax(np.abs(g - w)[ok] / lim[ok])))
+    g = {n: gu.to_np(x) for n, x in got.items()}
+    if where in ("dy", "dHT"):
+        assert not np.isfinite(g["dH0"][1, 2, :, col]).all() and not np.isfinite(g["dv"][1, :t - 63, 2, col]).any()
+        assert not np.isfinite(g["dk"][1, :t - 63, 2]).all(-1).any()
+    else:
+        assert not np.isfinite(g["HT"][1, 2, :, col]).all() and not np.isfinite(g["y"][1, t:, 2, col]).any()
