@@ -56,7 +56,7 @@ struct DeltaLayout {
   size_t states;  // one state per chunk
   size_t rows;    // U or Z of every step
   size_t exps;    // with the checkpoints: the powers of two of states and U (0: none)
-  size_t scales;  // powers of two of the gradients (0: none)
+  size_t dexps;   // powers of two of the gradients (0: none)
   size_t heads;   // dq or dk of every head in fp32 (0 where no heads share q, k)
 };
 

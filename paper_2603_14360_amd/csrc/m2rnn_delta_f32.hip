@@ -699,7 +699,7 @@ DeltaLayout delta_f32_layout(const DeltaArgs &a) {
   l.mats = align256(n * 2 * C * C * sizeof(float));
   l.states = align256(n * a.K * a.V * sizeof(float));
   l.rows = align256(steps * a.V * sizeof(float));
-  l.carry = l.exps = l.scales = 0;
+  l.carry = l.exps = l.dexps = 0;
   l.heads = a.N != a.Nqk ? align256(steps * a.K * sizeof(float)) : 0;
   return l;
 }

@@ -30,7 +30,7 @@ namespace {
 constexpr int C = 64;
 constexpr int LC = C + 8;       // halfs per row of an LDS array with a chunk's steps side by side
 // Floats per chunk: e^G, e^{G_C - G}, G / ln 2 as hi, lo, beta, and as ints at kTops the exponents (floor log2) of the
-// largest |k| and |beta|
+// largest |k|, |beta|, |P| and |q|
 constexpr int kTops = 5 * C, kGates = kTops + 16;
 // (Backward: e^G over om = 2^floor(G_0 / ln 2).  e^G goes into fp16 operands there, all of it can be as small as
 // the first step's gate, and the gradient of the state in front is then as small: om is put back in fp32.)
@@ -94,6 +94,16 @@ __device__ __forceinline__ float wave_top(F each) {
     top = group_max_nonneg<64>(top);
   }
   return top;
+}
+template <typename F, int M, int N>
+__device__ __forceinline__ void all_of(const f4_t (&x)[M][N], F put) {
+#pragma unroll
+  for (int i = 0; i < M * N * 4; ++i) put(x[i / (4 * N)][i / 4 % N][i % 4]);
+}
+template <typename F, int M>
+__device__ __forceinline__ void all_of(const f4_t (&x)[M], F put) {
+#pragma unroll
+  for (int i = 0; i < M * 4; ++i) put(x[i / 4][i % 4]);
 }
 // the exponent of the largest of four waves' tops, the same in all lanes and so in a scalar register; such that 2^e and
 // 2^-e are both normal numbers
@@ -160,7 +170,7 @@ __device__ __forceinline__ f4_t mma_f32(f4_t a, f4_t b, f4_t c) {
 // What bounds it is latency: all loads are issued at once, and 24 KB of LDS leave room for six workgroups per CU.
 // 8 x 4096 steps, 16 heads of 64 x 64: 65 us forward, 98 backward (3.5 TB/s, mostly of T and P).
 struct PrepLds {
-  float As[C][C + 4], Xt[C / 2][C / 2 + 4], hi[C], lo[C], be[C], tops[4];
+  float As[C][C + 4], Xt[C / 2][C / 2 + 4], hi[C], lo[C], be[C], tops[12];
 };
 template <int K, bool BWD>
 __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int unit, int ch, float *gates, half_t *mats,
@@ -209,16 +219,24 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int u
     const float top = wave_top([&](auto put) { put(beta); });
     if (lane == 0) ((int *)gt)[kTops + 1] = exponent_in_range(ilog2f(top));
   }
-  s2_t ktop = {kNoBf16Top, kNoBf16Top};
+  s2_t ktop = {kNoBf16Top, kNoBf16Top}, qtop = ktop;
 #pragma unroll
-  for (int e = 0; e < KB; ++e) ktop = bf16_top(kw[e], ktop);
-  const float kmax = group_max_nonneg<64>(bf16_top_value(ktop));
-  if (lane == 0) lds.tops[wv] = kmax;
+  for (int e = 0; e < KB; ++e) {
+    ktop = bf16_top(kw[e], ktop);
+    qtop = bf16_top(qw[e], qtop);
+  }
+  const float kmax = group_max_nonneg<64>(bf16_top_value(ktop)), qmax = group_max_nonneg<64>(bf16_top_value(qtop));
+  if (lane == 0) {
+    lds.tops[wv] = kmax;
+    lds.tops[4 + wv] = qmax;
+  }
   __syncthreads();
-  if (threadIdx.x == 0) ((int *)(gates + slot * kGates))[kTops] = exponent_of(*(const f4_t *)lds.tops);
-  u2_t ph[4], pl[4];  // P's four columns (rows, transposed) per tile: an operand's halves as they are
-#pragma unroll
-  for (int o = 0; o < 4; ++o) ph[o] = pl[o] = u2_t{0u, 0u};
+  if (threadIdx.x == 0) {
+    int *tops = (int *)(gates + slot * kGates) + kTops;
+    tops[0] = exponent_of(*(const f4_t *)lds.tops);
+    tops[3] = exponent_of(*(const f4_t *)(lds.tops + 4));
+  }
+  f4_t ps[4];  // P's four columns (rows, transposed) per tile
   const int mine = 16 * wv + d;
   auto tile = [&](int o, const u4_t *kt, const u4_t *qt) {
     f4_t kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
@@ -255,6 +273,18 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int u
           if (o - wv - 1 == x) p = tile(o, ko[x], qo[x]);
       }
     }
+    ps[o] = p;
+  }
+  const float pmax = wave_top([&](auto put) { all_of(ps, put); });
+  if (lane == 0) lds.tops[8 + wv] = pmax;
+  __syncthreads();
+  const int ep = exponent_of(*(const f4_t *)(lds.tops + 8));
+  if (threadIdx.x == 0) ((int *)(gates + slot * kGates))[kTops + 2] = ep;
+  // P over its largest entry, an operand's halves as they are
+  u2_t ph[4], pl[4];
+#pragma unroll
+  for (int o = 0; o < 4; ++o) {
+    const f4_t p = pow2i(-ep) * ps[o];
     if (BWD) {
       const Pair4 s = split4(p);
       ph[o] = s.hi;
@@ -263,7 +293,6 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int u
       ph[o] = pack4_h(p);
     }
   }
-  __syncthreads();
   if (lane < 16) {
     float x[16];
     float *A0 = &As[16 * wv][16 * wv];
@@ -432,7 +461,7 @@ struct Gates {
   static __device__ __forceinline__ uint32_t offset(int wv) {
     const int lane = threadIdx.x & 63, i = lane & 15;
     return 4 * (lane < 16 ? 16 * wv + i : lane < 32 ? C + 16 * wv + i : lane < 48 ? 4 * C + 16 * wv + i
-                : i == 0 ? C - 1 : i == 1 ? 2 * C : kTops + (i & 1));
+                : i == 0 ? C - 1 : i == 1 ? 2 * C : kTops + ((i - 2) & 3));
   }
   __device__ __forceinline__ f4_t four(int which) const { return *(const f4_t *)(at + 16 * which + 4 * ((threadIdx.x & 63) >> 4)); }
   __device__ __forceinline__ float one(int which) const { return at[16 * which + (threadIdx.x & 15)]; }
@@ -441,6 +470,8 @@ struct Gates {
   __device__ __forceinline__ int top(int i) const { return __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, at[50 + i])); }
   __device__ __forceinline__ int k_top() const { return top(0); }
   __device__ __forceinline__ int beta_top() const { return top(1); }
+  __device__ __forceinline__ int p_top() const { return top(2); }
+  __device__ __forceinline__ int q_top() const { return top(3); }
 };
 // A wave's 16 steps of VB columns, eight a lane as loaded, through LDS to four steps of one column per lane and
 // column tile, as in D[step][column]
@@ -465,16 +496,6 @@ constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC +
 
 // The largest |H| (upper 16 bits, cut to them as bf16) and |v| of a workgroup, infinities among them, in two halves of
 // a word: a word for every 16 lanes to LDS, and from there.
-template <typename F, int M, int N>
-__device__ __forceinline__ void all_of(const f4_t (&x)[M][N], F put) {
-#pragma unroll
-  for (int i = 0; i < M * N * 4; ++i) put(x[i / (4 * N)][i / 4 % N][i % 4]);
-}
-template <typename F, int M>
-__device__ __forceinline__ void all_of(const f4_t (&x)[M], F put) {
-#pragma unroll
-  for (int i = 0; i < M * 4; ++i) put(x[i / 4][i % 4]);
-}
 __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2_t, a), __builtin_bit_cast(us2_t, b)));
 }
@@ -502,6 +523,15 @@ __device__ __forceinline__ uint32_t top_of_all(const uint32_t *red) {
 }
 // the exponent of the lower 16 bits of x as bf16
 __device__ __forceinline__ int top_exponent(uint32_t x) { return max((int)(x >> 7 & 255u) - 127, -126); }
+// the same without what is not finite, as floats: four words of H, four of v
+template <int M, int N, int VT>
+__device__ __forceinline__ void finite_tops(uint32_t *red, const f4_t (&H)[M][N], const f4_t (&v)[VT], int wv) {
+  const float th = wave_top([&](auto put) { all_of(H, put); }), tw = wave_top([&](auto put) { all_of(v, put); });
+  if ((threadIdx.x & 63) == 0) {
+    red[wv] = __builtin_bit_cast(uint32_t, th);
+    red[4 + wv] = __builtin_bit_cast(uint32_t, tw);
+  }
+}
 __device__ __forceinline__ bool not_finite(uint32_t tops) {
   return (tops & 0x7F800000u) == 0x7F800000u || (tops & 0x7F80u) == 0x7F80u;
 }
@@ -593,7 +623,7 @@ __global__ void __launch_bounds__(256, 2)
   h8_t kf[KB];
   f4_t vf[VT], ge, gl, be;
   float g1, gc;
-  int ek, eb, eh = 0;
+  int ek, eb, ep, eh = 0;
   auto take1 = [&]() {
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
@@ -605,7 +635,7 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
     for (int t = 0; t < VT; ++t) vf[t] = tv.get(t);
     ge = gs.four(0); gl = gs.four(1); be = gs.four(2); g1 = gs.one(0); gc = gs.last();
-    ek = gs.k_top(); eb = gs.beta_top();
+    ek = gs.k_top(); eb = gs.beta_top(); ep = gs.p_top();
   };
   auto put_state = [&]() {
     if (S::on(wv))
@@ -643,11 +673,7 @@ __global__ void __launch_bounds__(256, 2)
   };
   // The exponents of the largest finite |H| and |v|
   auto measure = [&](int &et, int &ev) {
-    const float th = wave_top([&](auto put) { all_of(H, put); }), tw = wave_top([&](auto put) { all_of(vf, put); });
-    if (lane == 0) {
-      red[16 + wv] = __builtin_bit_cast(uint32_t, th);
-      red[20 + wv] = __builtin_bit_cast(uint32_t, tw);
-    }
+    finite_tops(red + 16, H, vf, wv);
     lds_barrier();
     et = eh + exponent_of(*(const u4_t *)(red + 16));
     ev = exponent_of(*(const u4_t *)(red + 20));
@@ -756,7 +782,7 @@ __global__ void __launch_bounds__(256, 2)
     lds_barrier();
     // H = e^{G_C} H + K^T W: D[row][column];  y = e^G (Q H)^T + (P U)^T
     h8_t wh[VTW][2], wl[VTW][2], uf[VT][2], us;
-    const float gy = pow2i(eh) * g1, ru = pow2i(er), rus = pow2i(er - eh);
+    const float gy = pow2i(eh) * g1, rp = pow2i(er + ep), rus = pow2i(er - eh);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -806,7 +832,7 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
         settle(u[t]);
-        y[t] = gy * y[t] + ru * u[t];
+        y[t] = gy * y[t] + rp * u[t];
       }
     }
     if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
@@ -839,24 +865,23 @@ __global__ void __launch_bounds__(256, 2)
           p.HT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] = H[i][j][x];
 }
 
-// Backward, chunks in reverse order.  Gradients of a chunk are brought near one by s, a power of two from the
-// largest |dH| and |dy| of the workgroup's columns: with unit keys nothing below exceeds some hundreds then, and
-// the pairs' 2^-25 is small.  8 x 4096 steps, 16 heads of 64 x 64: 235 us, 3.7 a chunk (3.5 TB/s).
+// Backward, chunks in reverse order.  As in the forward dH lies in registers over 2^ed and enters as that, dy over 2^ey,
+// from the largest ones of the workgroup's columns; dU and Z are over 2^ez, from a bound of the terms of dU (Z is not
+// much larger while the rule does not expand).  8 x 4096 steps, 16 heads of 64 x 64: 235 us, 3.7 a chunk (3.5 TB/s).
 template <int K, int VB>
-constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 16; }
+constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 7 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 24 * 4; }
 
 template <int K, int VB>
 __global__ void __launch_bounds__(256, 2)
     delta_half_bwd_kernel(DeltaArgs a, int chunks, const float *__restrict__ gates, const half_t *__restrict__ mats,
-                          half_t *__restrict__ dstates, half_t *__restrict__ rows_z, float *__restrict__ scales) {
+                          half_t *__restrict__ dstates, half_t *__restrict__ rows_z, u4_t *__restrict__ exps) {
   using S = Scan<K, VB>;
   constexpr int KB = S::KB, KT = S::KT, VT = S::VT, KTW = S::KTW, VTW = S::VTW, LK = S::LK;
   extern __shared__ __align__(16) char lds[];
   half_t *ks = (half_t *)lds, *qs = ks + C * LK, *Ht = qs + C * LK, *Hl = Ht + VB * LK, *Yt = Hl + VB * LK;
   half_t *Wt = Yt + VB * LC, *Wl = Wt + VB * LC, *Ut = Wl + VB * LC, *Ul = Ut + VB * LC;
-  half_t *Zt = Wt, *Zl = Wl;  // (W has been read when Z comes)
-  half_t *turn = Ul + VB * LC;
-  float *red = (float *)(turn + 4 * Turn<VB>::HALFS) + 4 * 64;
+  half_t *Zt = Ul + VB * LC, *Zl = Zt + VB * LC, *turn = Zl + VB * LC;
+  uint32_t *red = (uint32_t *)(turn + 4 * Turn<VB>::HALFS) + 4 * 64;
   int unit, part;
   if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -878,6 +903,11 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         D[i][j][x] = a.dHT ? a.dHT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
+  // (here, and not at the head of the loop, which would then wait for everything in each of its rounds)
+#pragma unroll
+  for (int i = 0; i < KTW; ++i)
+#pragma unroll
+    for (int j = 0; j < VTW; ++j) settle(D[i][j]);
   u4_t nk[KB], nq[KB], ny;
   h8_t Tf[4], Pf[4];  // [32 steps, the later ones first][hi, lo]
   float ng;
@@ -904,6 +934,7 @@ __global__ void __launch_bounds__(256, 2)
   h8_t kf[KB], qf[KB];
   f4_t yf[VT], ge, gl, be;
   float b1, gc, om;
+  int ek, eb, ep, eq, ed = 0, ey = 0;
   auto take1 = [&]() {
     ty.put(ny);
     gs.at[lane] = ng;
@@ -919,36 +950,17 @@ __global__ void __launch_bounds__(256, 2)
     ge = gs.four(0); gl = gs.four(1); be = gs.four(2); b1 = gs.one(2);
     om = gate_unit(gs.first());
     gc = om * gs.last();
+    ek = gs.k_top(); eb = gs.beta_top(); ep = gs.p_top(); eq = gs.q_top();
   };
-  if (chunks > 0) {
-    fetch1(chunks - 1);
-    fetch2(chunks - 1);
-    fetch3(chunks - 1);
-    take1();
-  }
   const int w = place(wv);
-  for (int ch = chunks - 1; ch >= 0; --ch) {
-    const int next = max(ch - 1, 0);
-    const float top = wave_top([&](auto put) {
-      all_of(yf, put);
-      all_of(D, put);
-    });
-    if (lane == 0) red[wv] = top;
-    lds_barrier();  // (and everything of the chunk before has been read)
-    const f4_t tops = *(const f4_t *)red;
-#pragma unroll
-    for (int i = 0; i < KB; ++i) {
-      *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
-      *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = qf[i];
-    }
-    const int e = exponent_of(tops);
-    const float s = pow2i(-e), inv = pow2i(e);
+  auto put_in = [&]() {
+    const float sy = pow2i(-ey);
     if (S::on(wv))
 #pragma unroll
       for (int i = 0; i < KTW; ++i)
 #pragma unroll
         for (int j = 0; j < VTW; ++j) {
-          const Pair4 x = split4(s * D[i][j]);
+          const Pair4 x = split4(D[i][j]);
           const int o = (16 * S::vt(wv, j) + d) * LK + 16 * S::kt(wv, i) + 4 * g4;
           *(u2_t *)&Ht[o] = x.hi;
           *(u2_t *)&Hl[o] = x.lo;
@@ -956,58 +968,119 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       const int o = (16 * t + d) * LC + w;
-      const f4_t y = s * yf[t];
+      const f4_t y = sy * yf[t];
       const Pair4 x = split4(ge * y);
       *(u2_t *)&Yt[o] = pack4_h(y);
       *(u2_t *)&Wt[o] = x.hi;
       *(u2_t *)&Wl[o] = x.lo;
     }
+  };
+  // From the exponents of the largest |dH| and |dy|, that of dU, and that to scale dH with: dH counts as no smaller
+  // than 2^-24 of what the chunk adds to it.
+  auto scale_for = [&](int td, int ty, int &ez) {
+    ez = exponent_in_range(max(td + ek, ty + ep));
+    return max(exponent_in_range(td), exponent_in_range(max(ty + eq, ez + eb + ek)) - 24);
+  };
+  auto measure = [&](int &td, int &ty) {
+    finite_tops(red + 16, D, yf, wv);
     lds_barrier();
+    td = ed + exponent_of(*(const u4_t *)(red + 16));
+    ty = exponent_of(*(const u4_t *)(red + 20));
+  };
+  auto rescale = [&](int to) {
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) D[i][j][x] = __builtin_amdgcn_ldexpf(D[i][j][x], ed - to);
+    ed = to;
+  };
+  if (chunks > 0) {
+    fetch1(chunks - 1);
+    fetch2(chunks - 1);
+    fetch3(chunks - 1);
+    take1();
+    int td, ez;
+    measure(td, ey);
+    rescale(scale_for(td, ey, ez));
+  }
+  for (int ch = chunks - 1; ch >= 0; --ch) {
+    const int next = max(ch - 1, 0);
+    put_in();
+#pragma unroll
+    for (int i = 0; i < KB; ++i) {
+      *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
+      *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = qf[i];
+    }
+    top_of_rows(red, D, yf, wv);
+    lds_barrier();  // (of the chunk before only Z may still be read)
     // dU = P^T dY + e^{G_C - G} K dH: D[step][column]
+    const uint32_t tops = top_of_all(red);
     h8_t hh[VT][KB], hl[VT][KB], yy[VT][2];
+    auto get_in = [&]() {
 #pragma unroll
-    for (int i = 0; i < KB; ++i)
+      for (int i = 0; i < KB; ++i)
 #pragma unroll
-      for (int t = 0; t < VT; ++t) {
-        const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
-        hh[t][i] = ld8(Ht + o);
-        hl[t][i] = ld8(Hl + o);
-      }
+        for (int t = 0; t < VT; ++t) {
+          const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
+          hh[t][i] = ld8(Ht + o);
+          hl[t][i] = ld8(Hl + o);
+        }
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int t = 0; t < VT; ++t) yy[t][kb] = ld8(Yt + (16 * t + d) * LC + 32 * kb + 8 * g4);
-    fetch1(next);
+        for (int t = 0; t < VT; ++t) yy[t][kb] = ld8(Yt + (16 * t + d) * LC + 32 * kb + 8 * g4);
+    };
     f4_t u[VT], ul[VT], py[VT];
+    auto products = [&]() {
 #pragma unroll
-    for (int t = 0; t < VT; ++t) u[t] = ul[t] = py[t] = zero;
+      for (int t = 0; t < VT; ++t) u[t] = ul[t] = py[t] = zero;
 #pragma unroll
-    for (int i = 0; i < KB; ++i)
+      for (int i = 0; i < KB; ++i)
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          u[t] = mfma_k32(kf[i], hh[t][i], u[t]);
+          ul[t] = mfma_k32(kf[i], hl[t][i], ul[t]);
+        }
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
-        u[t] = mfma_k32(kf[i], hh[t][i], u[t]);
-        ul[t] = mfma_k32(kf[i], hl[t][i], ul[t]);
+        py[t] = mfma_k32(Pf[0], yy[t][1], py[t]);
+        py[t] = mfma_k32(Pf[1], yy[t][1], py[t]);
+        py[t] = mfma_k32(Pf[2], yy[t][0], py[t]);
+        py[t] = mfma_k32(Pf[3], yy[t][0], py[t]);
       }
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      py[t] = mfma_k32(Pf[0], yy[t][1], py[t]);
-      py[t] = mfma_k32(Pf[1], yy[t][1], py[t]);
-      py[t] = mfma_k32(Pf[2], yy[t][0], py[t]);
-      py[t] = mfma_k32(Pf[3], yy[t][0], py[t]);
+    };
+    get_in();
+    fetch1(next);
+    products();
+    int td = ed + top_exponent(tops >> 16), ty_ = top_exponent(tops), ez;
+    int want = scale_for(td, ty_, ez);
+    if (not_finite(tops) || want < ed - 2 || want > ed + 13 || ty_ < ey - 2 || ty_ > ey + 13) {  // (the same in all waves)
+      measure(td, ty_);
+      want = scale_for(td, ty_, ez);
+      rescale(want);
+      ey = ty_;
+      put_in();
+      lds_barrier();
+      get_in();
+      products();
     }
     hold();
     fetch2(next);
     hold();
+    const f4_t glz = pow2i(ed - ez) * gl;
+    const float pz = pow2i(ey + ep - ez);
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       settle(u[t]);
       settle(ul[t]);
       settle(py[t]);
-      const Pair4 x = split4(gl * (u[t] + ul[t]) + py[t]);
+      const Pair4 x = split4(glz * (u[t] + ul[t]) + pz * py[t]);
       *(u2_t *)&Ut[(16 * t + d) * LC + w] = x.hi;
       *(u2_t *)&Ul[(16 * t + d) * LC + w] = x.lo;
     }
-    // (what Q^T e^G dY needs, before Z takes W's place)
+    // (what Q^T e^G dY needs)
     h8_t hs[KTW], xT[KTW][2], wh[VTW][2], wl[VTW][2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -1055,7 +1128,7 @@ __global__ void __launch_bounds__(256, 2)
       xl[t] = mfma_k32(Tf[3], uh[t][0], xl[t]);
       xl[t] = mfma_k32(Tf[2], uo[t][0], xl[t]);
     }
-    const f4_t bg = -(be * ge);
+    const f4_t bg = -pow2i(-eb) * (be * ge);
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       settle(x[t]);
@@ -1091,14 +1164,21 @@ __global__ void __launch_bounds__(256, 2)
     hold();
 #pragma unroll
     for (int t = 0; t < VT; ++t) settle(z[t]);
-    const float back = inv * om;
+    const float backq = om * pow2i(ey - ed), backk = om * pow2i(ez + eb - ed);
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) {
+        settle(acc[i][j]);
+        D[i][j] = gc * D[i][j] + backq * acc[i][j];
+      }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < KTW; ++i)
 #pragma unroll
         for (int j = 0; j < VTW; ++j) {
-          acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], acc[i][j]);
+          acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], kb ? acc[i][j] : zero);
           acc[i][j] = mfma_k32(xT[i][kb], wh[j][kb], acc[i][j]);
         }
 #pragma unroll
@@ -1106,9 +1186,9 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int j = 0; j < VTW; ++j) {
         settle(acc[i][j]);
-        D[i][j] = gc * D[i][j] + back * acc[i][j];
+        D[i][j] += backk * acc[i][j];
       }
-    const float bz = b1 * inv;
+    const float bz = b1 * pow2i(ez);
     take1();
     const size_t at = (size_t)unit * chunks + ch;
     const auto o = in.o.at(ch);
@@ -1123,8 +1203,11 @@ __global__ void __launch_bounds__(256, 2)
     if (KT >= 4 || wv < KT)
 #pragma unroll
       for (int i = 0; i < KTW; ++i) *(h8_t *)(dstates + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
-    if (threadIdx.x == 0) scales[at * (a.V / VB) + part] = s;
+    // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
+    __builtin_amdgcn_raw_buffer_store_b128(u4_t{(uint32_t)ed, (uint32_t)ez, (uint32_t)ey, 0u}, __builtin_amdgcn_make_buffer_rsrc(
+                                           exps + at * (a.V / VB) + part, 0, 16, 0x00027000), 16 * (int)threadIdx.x, 0, 0);
   }
+  rescale(0);
   if (a.dH0 && S::on(wv))
 #pragma unroll
     for (int i = 0; i < KTW; ++i)
@@ -1166,7 +1249,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
     delta_half_grad_kernel(DeltaArgs a, int chunks, int vbs, const float *__restrict__ gates,
                            const half_t *__restrict__ states, const half_t *__restrict__ rows_u,
                            const int *__restrict__ exps, const half_t *__restrict__ dstates, const half_t *__restrict__ rows_z,
-                           const float *__restrict__ scales, float *__restrict__ dq_heads, float *__restrict__ dk_heads) {
+                           const u4_t *__restrict__ dexps, float *__restrict__ dq_heads, float *__restrict__ dk_heads) {
   constexpr int KB = K / 32, KT = K / 16, LK = K + 8;
   constexpr bool ONE = V32 > 2;
   extern __shared__ __align__(16) char lds[];
@@ -1191,27 +1274,24 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   }
   const half_t *U = rows_u + at * C * a.V + lane * 8, *Z = rows_z + at * C * a.V + (size_t)wv * 512 + lane * 8;
   const half_t *h0 = states + at * K * a.V + lane * 8, *h1 = dstates + at * K * a.V + lane * 8;
-  // States and U of a block of columns (one of `blocks`) come with a power of two of their own; the chunk's common one is
-  // the largest.  Lanes below 16 have the blocks' factors to it of the states, the next 16 of U.
-  const int blocks = a.V / vbs;
-  const bool mine = lane < 32 && (lane & 15) < blocks;
-  const int el = mine ? exps[(at * blocks + (lane & 15)) * 2 + (lane >> 4)] : -1000;
-  const int et = __builtin_bit_cast(int, group_max_nonneg<16>(__builtin_bit_cast(float, el + 1000))) - 1000;
+  // What comes for a block of columns (one of `blocks`) has a power of two of its own; the chunk's common one is the
+  // largest.  Each 16 lanes have the blocks' factors to it: of the states, of U, of dH and of Z.
+  const int blocks = a.V / vbs, lb = lane & 15;
+  const bool there = lb < blocks;
+  const int ey = there ? (int)dexps[at * blocks + lb][2] : -1000;
+  const int el = !there ? -1000 : lane < 32 ? exps[(at * blocks + lb) * 2 + (lane >> 4)] : (int)dexps[at * blocks + lb][(lane >> 4) - 2];
+  auto row_top = [](int e) { return __builtin_bit_cast(int, group_max_nonneg<16>(__builtin_bit_cast(float, e + 1000))) - 1000; };
+  const int et = row_top(el), eY = __builtin_amdgcn_readlane(row_top(ey), 0);
   const int eh = __builtin_amdgcn_readlane(et, 0), eu = __builtin_amdgcn_readlane(et, 16);
+  const int eD = __builtin_amdgcn_readlane(et, 32), eZ = __builtin_amdgcn_readlane(et, 48);
   const int fl = __builtin_bit_cast(unsigned short, (half_t)pow2i(el - et));
   auto own_factor = [&](int kind, int vb) {
     const half_t f = __builtin_bit_cast(half_t, (unsigned short)__shfl(fl, 16 * kind + (vbs == 32 ? vb : 2 * vb + (g4 >> 1)), 64));
     return h8_t{f, f, f, f, f, f, f, f};
   };
-  // the gradients' common power of two: that of the block with the largest
-  const float *sb = scales + at * blocks;
-  float sc = sb[0];
-  for (int x = 1; x < blocks; ++x) sc = fminf(sc, sb[x]);
-  auto factor = [&](int vb) {  // brings a block of 32 columns of Z or dH to it
-    const float s = vbs == 32 ? sb[vb] : g4 < 2 ? sb[2 * vb] : sb[2 * vb + 1];
-    const half_t f = (half_t)(sc * __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, s)));  // sc / s
-    return h8_t{f, f, f, f, f, f, f, f};
-  };
+  const int *gt_tops = (const int *)gates + at * kGates + kTops;
+  const int eb = gt_tops[1];
+  const float sy = pow2i(-eY), sb = pow2i(-eb);
 
 #pragma unroll
   for (int e = 0; e < KB; ++e) {
@@ -1221,7 +1301,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   for (int x = threadIdx.x; x < kTops; x += 256) {
     const float g = gates[at * kGates + x];
     ge[x] = g;
-    if (x >= 4 * C) bh[x - 4 * C] = (half_t)g;
+    if (x >= 4 * C) bh[x - 4 * C] = (half_t)(sb * g);
   }
 
   f4_t s1[4], s2[4], dq[KT], as[KT], kept[KT];
@@ -1230,8 +1310,8 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
 #pragma unroll
   for (int x = 0; x < KT; ++x) dq[x] = as[x] = kept[x] = zero;
   float zv = 0.f, hd = 0.f;
-  auto with_states = [&](int vb, h8_t f8, h8_t y, h8_t z, h8_t u) {
-    const h8_t uf = u * (f8 * own_factor(1, vb));  // (f8: for dH, whose power of two it is)
+  auto with_states = [&](int vb, h8_t y, h8_t z, h8_t u) {
+    const h8_t fd = own_factor(2, vb), uf = u * (fd * own_factor(1, vb));
     const h8_t fh = own_factor(0, vb), yh = y * fh, zh = z * fh;
     float hb = 0.f;
 #pragma unroll
@@ -1242,13 +1322,13 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
       kept[x] = mfma_k32(x1, uf, kept[x]);
       if ((x & 3) == wv) hb = dot8(x0, x1, hb);
     }
-    hd = fmaf((float)f8[0] * (float)fh[0], hb, hd);
+    hd = fmaf((float)fd[0] * (float)fh[0], hb, hd);
   };
 #pragma unroll
   for (int vb = 0; vb < (ONE ? 1 : V32); ++vb)
 #pragma unroll 1
     for (int vo = vb; vo < (ONE ? V32 : vb + 1); ++vo) {
-      const h8_t f8 = factor(vo), z = ld8(Z + vo * 2048) * f8, y = bf16_to_h8(buf_ld(ry, ov + 64 * vo), sc);
+      const h8_t z = ld8(Z + vo * 2048) * own_factor(3, vo), y = bf16_to_h8(buf_ld(ry, ov + 64 * vo), sy);
       float vv[8];
       bf16x8_to_f32(buf_ld(rv, ov + 64 * vo), vv);
 #pragma unroll
@@ -1262,7 +1342,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
         s1[j] = mfma_k32(u, yu, s1[j]);
         s2[j] = mfma_k32(u, zu, s2[j]);
       }
-      if (ONE) with_states(vo, f8, y, z, u);  // (the last u is my own)
+      if (ONE) with_states(vo, y, z, u);  // (the last u is my own)
     }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -1316,8 +1396,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   if (!ONE)
 #pragma unroll
     for (int vb = 0; vb < V32; ++vb) {
-      const h8_t f8 = factor(vb);
-      with_states(vb, f8, bf16_to_h8(buf_ld(ry, ov + 64 * vb), sc), ld8(Z + vb * 2048) * f8, ld8(U + (vb * 4 + wv) * 512));
+      with_states(vb, bf16_to_h8(buf_ld(ry, ov + 64 * vb), sy), ld8(Z + vb * 2048) * own_factor(3, vb), ld8(U + (vb * 4 + wv) * 512));
     }
 #pragma unroll
   for (int x = 0; x < KT; ++x) {
@@ -1331,10 +1410,8 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   __syncthreads();
   const bool heads = a.N != a.Nqk;
   // every product with the powers of two that its factors came without
-  const int es = -ilog2f(sc), eY = es, eZ = es, eD = es;
-  const float inv = pow2i(eZ);
   const float cq = gm * pow2i(eh + eY), ca = -gm * pow2i(eh + eZ), ck = gt * pow2i(eu + eD);
-  const float c1 = pow2i(x1 + eu + eY), c2 = pow2i(x2 + eu + eZ);
+  const float c1 = pow2i(x1 + eu + eY), c2 = pow2i(x2 + eu + eZ), cb = pow2i(x2 + eu + eZ + eb);
   float dG = 0.f, kb1 = 0.f, tail = 0.f;
   h8_t row1[2], row2[2], col1[2], colb[2];
 #pragma unroll
@@ -1367,7 +1444,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
       const float qx = (float)qv[r], kx = (float)kv[r];
       x[r] = fmaf(c1, x[r], cq * dq[kt][r]);
       y[r] = fmaf(c2, y[r], ca * as[kt][r]);
-      w[r] = fmaf(c1, w[r], fmaf(c2, wb[r], ck * kd[r]));
+      w[r] = fmaf(c1, w[r], fmaf(cb, wb[r], ck * kd[r]));
       o[r] = fmaf(bt, y[r], w[r]);
       dG = fmaf(qx, x[r], dG);
       dG = fmaf(kx, fmaf(bt, y[r], -w[r]), dG);
@@ -1394,7 +1471,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   if (lane == 0) red[12 + wv] = tail;
   if (g4 == 0) red[16 + i] = dG;
   if (g4 == 0 && own < a.T)
-    ((__hip_bfloat16 *)a.dbeta)[((size_t)b * a.T + own) * a.N + n] = __float2bfloat16(inv * zv + kb1);
+    ((__hip_bfloat16 *)a.dbeta)[((size_t)b * a.T + own) * a.N + n] = __float2bfloat16(pow2i(eZ) * zv + kb1);
   __syncthreads();
   if (wv == 0) {  // sums over the steps behind, in 64 bits; <H_C, dH> at the last one
     double s = (double)red[16 + lane];
@@ -1428,7 +1505,8 @@ __global__ void __launch_bounds__(256)
 struct Ws {
   float *gates, *carry;
   half_t *mats, *dstates, *rows_z;
-  float *scales, *dqh, *dkh;
+  u4_t *exps;
+  float *dqh, *dkh;
 };
 Ws carve(const DeltaLayout &l, char *p) {
   Ws w;
@@ -1437,8 +1515,8 @@ Ws carve(const DeltaLayout &l, char *p) {
   w.carry = (float *)(p += l.mats);
   w.dstates = (half_t *)(p += l.carry);
   w.rows_z = (half_t *)(p += l.states);
-  w.scales = (float *)(p += l.rows);
-  w.dqh = (float *)(p += l.scales);
+  w.exps = (u4_t *)(p += l.rows);
+  w.dqh = (float *)(p += l.dexps);
   w.dkh = (float *)(p += l.heads);
   return w;
 }
@@ -1503,7 +1581,7 @@ hipError_t grad_go(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, int vb
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((delta_half_grad_kernel<K, V32>), dim3((unsigned)(a.B * a.N) * (unsigned)l.chunks), dim3(256), lds, s,
                      a, l.chunks, vb, w.gates, (const half_t *)a.ckpt, (const half_t *)(a.ckpt + l.states),
-                     (const int *)(a.ckpt + l.states + l.rows), w.dstates, w.rows_z, w.scales, w.dqh, w.dkh);
+                     (const int *)(a.ckpt + l.states + l.rows), w.dstates, w.rows_z, w.exps, w.dqh, w.dkh);
   return hipGetLastError();
 }
 template <int K, int VB>
@@ -1511,7 +1589,7 @@ hipError_t bwd_kv(const DeltaArgs &a, const DeltaLayout &l, const Ws &w, hipStre
   constexpr int lds = lds_bwd<K, VB>();
   hipError_t e = set_max_lds_once(delta_half_bwd_kernel<K, VB>, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((delta_half_bwd_kernel<K, VB>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a, l.chunks, w.gates, w.mats, w.dstates, w.rows_z, w.scales);
+  hipLaunchKernelGGL((delta_half_bwd_kernel<K, VB>), dim3(delta_grid(a.B * a.N, a.V / VB)), dim3(256), lds, s, a, l.chunks, w.gates, w.mats, w.dstates, w.rows_z, w.exps);
   if ((e = hipGetLastError()) != hipSuccess || l.chunks == 0) return e;
   switch (a.V) {
     case 32: return grad_go<K, 1>(a, l, w, VB, s);
@@ -1549,7 +1627,7 @@ DeltaLayout delta_half_layout(const DeltaArgs &a) {
   l.states = align256(n * a.K * a.V * sizeof(half_t));
   l.rows = align256(n * C * a.V * sizeof(half_t));
   l.exps = align256(n * (a.V / 16) * 2 * sizeof(int));
-  l.scales = align256(n * (a.V / 16) * sizeof(float));
+  l.dexps = align256(n * (a.V / 16) * sizeof(u4_t));
   l.heads = a.N != a.Nqk ? align256(steps * a.K * sizeof(float)) : 0;
   return l;
 }

@@ -40,6 +40,52 @@ def test_values_and_states_of_any_size(io, B, T, N, K, V):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,N,K,V", SIZES)
+def test_gradients_of_any_size(io, B, T, N, K, V):
+    """From 2^-60 to 2^110: the results are linear in (dy, dHT)."""
+    s = dr.rule_inputs(64, B, T, N, K, V, io=io)
+    base = small.run(s, io)
+    for e in (-60, -20, 13, 60, 110):
+        print("case", io, B, T, N, K, V, e, flush=True)
+        got = small.run(times(s, dy=e, dHT=e), io, use_ckpt=e != 13)
+        same_but_for(got, base, **dict.fromkeys(("dq", "dk", "dv", "dg", "dbeta", "dH0"), e))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,N,K,V", SIZES)
+def test_large_queries(io, B, T, N, K, V):
+    """(Entries of q far below its largest are not exact as fp16, so the bits differ.)"""
+    s = times(dr.rule_inputs(65, B, T, N, K, V, io=io), q=13, dHT=13)
+    small.check(small.run(s, io), dr.rule(s), (io, B, T, N, K, V))
+
+
+@pytest.mark.parametrize("T", [13, 65, 130])
+def test_queries_that_add_up(T):
+    """Products q.k of thousands, the same query and loss at every step: dU is the sum of all of them."""
+    s = dr.rule_inputs(66, 2, T, 3, 64, 64, io="bf16")
+    s["k"][:, ::2] = 0.125
+    s["q"][:] = 1000
+    s["dy"][:] = 1
+    s["g"][:] = s["g"] * np.float32(0.05)
+    want, got = dr.rule(s), small.run(s, "bf16")
+    # the aligned keys take most of Q^T e^G dY away again: dH0 is the difference of it and K^T e^G dV, sums over a
+    # chunk of up to sum_t |q_t dy_t| an entry, each off by F32 of that
+    err = np.abs(gu.to_np(got["dH0"]) - want.pop("dH0")).max()
+    assert err <= small.F32 * 1000 * min(T, 64), err
+    small.check(got, want, T)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("e", [20, 60])
+def test_dq_beside_a_large_gradient_of_the_state(io, e):
+    """dq_t = H_t dy_t has nothing to do with dHT."""
+    s = dr.rule_inputs(67, 2, 100, 3, 64, 64, io=io)
+    base, got = small.run(s, io), small.run(times(s, dHT=e), io)
+    import torch
+    assert torch.equal(got["dq"], base["dq"])
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("T", [12, 13, 65, 130])
 @pytest.mark.parametrize("size", [1e4, 1.9e4])
 def test_a_state_along_a_key(io, T, size):
