@@ -7,11 +7,14 @@
 //   delta_half_bwd_kernel    the same, backwards                                  -> dv, dH0, dH and Z
 //   delta_half_grad_kernel   one workgroup per chunk                              -> dq, dk, dg, dbeta
 //
-// Operands.  q, k, v, dy are bf16 and exact as fp16 (magnitudes from 2^-17 to 2^15).  Everything that reaches a
+// Operands.  q, k, v, dy are bf16 and exact as fp16 beside the largest of their chunk.  Everything that reaches a
 // state enters its product as an fp16 pair hi + lo of 22 bits, so that states and their gradients, which are
 // fp32, are as good as that; what only reaches a bf16 result is one fp16 value of 11 bits.  T is formed in fp32.
-// The rule is linear in v and H, and its gradients in dy and dH: a chunk's state, its R and U, and its gradients are
-// brought near one by powers of two first, per workgroup, and may have any magnitude.
+//
+// Powers of two.  No magnitude is given, and fp16 has few exponents: every operand is brought near one by a power of two of
+// its chunk (H, U, dH, dy, Z: of its workgroup's columns too), which its products are given back in fp32.  They come
+// from the largest finite entries of q, k, beta and P (found with T) and of v, H, dy and dH (by the chains), and
+// of sums, U and Z, from bounds that hold while the rule does not expand.  What is below 2^-25 of the largest is lost.
 //
 // Layout.  Products are D = A B^T: a lane gives eight elements of row (lane % 16) of a factor, and holds rows
 // 4 (lane / 16) .. + 3 of column lane % 16 of D.  Which eight of the 32 that are contracted is free, as long as both
@@ -23,6 +26,7 @@
 #include "m2rnn_delta.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace m2rnn {
 namespace {
@@ -49,6 +53,18 @@ __device__ __forceinline__ uint32_t pack2_h(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, h2_t));
 }
 __device__ __forceinline__ u2_t pack4_h(f4_t x) { return u2_t{pack2_h(x[0], x[1]), pack2_h(x[2], x[3])}; }
+// 2^e, no more than 2^127
+__device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.f, min(e, 127)); }
+// eight bf16 values times s, as fp16
+__device__ __forceinline__ h8_t bf16_to_h8(u4_t w, float s) {
+  u4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = w[i];
+    r[i] = pack2_h(s * __builtin_bit_cast(float, x << 16), s * __builtin_bit_cast(float, x & 0xFFFF0000u));
+  }
+  return __builtin_bit_cast(h8_t, r);
+}
 // eight bf16 values as fp16
 __device__ __forceinline__ h8_t bf16_to_h8(u4_t w) {
   u4_t r;
@@ -58,6 +74,20 @@ __device__ __forceinline__ h8_t bf16_to_h8(u4_t w) {
     r[i] = pack2_h(__builtin_bit_cast(float, x << 16), __builtin_bit_cast(float, x & 0xFFFF0000u));
   }
   return __builtin_bit_cast(h8_t, r);
+}
+// Keys and queries of a chunk whose largest entry has an exponent e far from zero come as fp16 over 2^e, others as they
+// are: entries of 2^-17 and more are exact then, and of keys 2^-21 of the largest one is lost at most, of queries,
+// which reach nothing but bf16 results and dH0, 2^-15.
+__device__ __forceinline__ bool far_key(int e) { return e < -4 || e > 10; }
+__device__ __forceinline__ bool far_query(int e) { return e < -10 || e > 10; }
+template <bool FAR, int N>
+__device__ __forceinline__ void rows_to_h8(const u4_t (&w)[N], int e, h8_t (&x)[N]) {
+  const float s = two_to(-e);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = FAR ? bf16_to_h8(w[i], s) : bf16_to_h8(w[i]);
+}
+__device__ __forceinline__ f4_t fma4(float a, f4_t b, f4_t c) {
+  return f4_t{fmaf(a, b[0], c[0]), fmaf(a, b[1], c[1]), fmaf(a, b[2], c[2]), fmaf(a, b[3], c[3])};
 }
 // four floats as fp16 hi and lo parts
 struct Pair4 {
@@ -284,7 +314,7 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int u
   u2_t ph[4], pl[4];
 #pragma unroll
   for (int o = 0; o < 4; ++o) {
-    const f4_t p = pow2i(-ep) * ps[o];
+    const f4_t p = two_to(-ep) * ps[o];
     if (BWD) {
       const Pair4 s = split4(p);
       ph[o] = s.hi;
@@ -467,11 +497,8 @@ struct Gates {
   __device__ __forceinline__ float one(int which) const { return at[16 * which + (threadIdx.x & 15)]; }
   __device__ __forceinline__ float last() const { return at[48]; }    // e^G of the chunk's last step
   __device__ __forceinline__ float first() const { return at[49]; }   // hi of its first
-  __device__ __forceinline__ int top(int i) const { return __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, at[50 + i])); }
-  __device__ __forceinline__ int k_top() const { return top(0); }
-  __device__ __forceinline__ int beta_top() const { return top(1); }
-  __device__ __forceinline__ int p_top() const { return top(2); }
-  __device__ __forceinline__ int q_top() const { return top(3); }
+  // (the tops from the lanes that have loaded them)
+  static __device__ __forceinline__ int top(float x, int i) { return __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 50 + i); }
 };
 // A wave's 16 steps of VB columns, eight a lane as loaded, through LDS to four steps of one column per lane and
 // column tile, as in D[step][column]
@@ -492,15 +519,15 @@ struct Turn {
 };
 
 template <int K, int VB>
-constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 24 * 4; }
+constexpr int lds_fwd() { return (C * (K + 8) + 2 * VB * (K + 8) + 5 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 12 * 4; }
 
 // The largest |H| (upper 16 bits, cut to them as bf16) and |v| of a workgroup, infinities among them, in two halves of
-// a word: a word for every 16 lanes to LDS, and from there.
+// a word, a word for every wave, to LDS and from there.
 __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2_t, a), __builtin_bit_cast(us2_t, b)));
 }
 template <int M, int N, int VT>
-__device__ __forceinline__ void top_of_rows(uint32_t *red, const f4_t (&H)[M][N], const f4_t (&v)[VT], int wv) {
+__device__ __forceinline__ void top_of_wave(uint32_t *red, const f4_t (&H)[M][N], const f4_t (&v)[VT], int wv) {
   float th = 0.f, tw = 0.f;
   all_of(H, [&](float x) { th = fmaxf(th, fabsf(x)); });
   all_of(v, [&](float x) { tw = fmaxf(tw, fabsf(x)); });
@@ -509,16 +536,12 @@ __device__ __forceinline__ void top_of_rows(uint32_t *red, const f4_t (&H)[M][N]
   t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
   t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x141, 0xF, 0xF, false));  // row_half_mirror
   t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x140, 0xF, 0xF, false));  // row_mirror
-  if ((threadIdx.x & 15) == 0) red[4 * wv + ((threadIdx.x & 63) >> 4)] = t;
+  t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x142, 0xA, 0xF, false));  // row_bcast:15: rows 1 and 3 also those before
+  t = max_halves(t, __builtin_amdgcn_update_dpp(0, t, 0x143, 0xC, 0xF, false));  // row_bcast:31: the last row all
+  if ((threadIdx.x & 63) == 63) red[wv] = t;
 }
 __device__ __forceinline__ uint32_t top_of_all(const uint32_t *red) {
-  u4_t m = *(const u4_t *)red;
-#pragma unroll
-  for (int i = 1; i < 4; ++i) {
-    const u4_t x = *(const u4_t *)(red + 4 * i);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = max_halves(m[j], x[j]);
-  }
+  const u4_t m = *(const u4_t *)red;
   return __builtin_amdgcn_readfirstlane(max_halves(max_halves(m[0], m[1]), max_halves(m[2], m[3])));
 }
 // the exponent of the lower 16 bits of x as bf16
@@ -536,10 +559,10 @@ __device__ __forceinline__ bool not_finite(uint32_t tops) {
   return (tops & 0x7F800000u) == 0x7F800000u || (tops & 0x7F80u) == 0x7F80u;
 }
 
-// Forward.  The state lies in registers over 2^eh, which stays while its largest entry is between 2^-2 and 2^13 of
-// that; R and U are over 2^er, from the chunk's largest |H|, |v|, |k| and |beta|.  The largest |H| is known to all waves
-// only behind the barrier that hands the state over: a state that has left its range is then handed over again, scaled anew
-// (which a sequence does a few times at its start).
+// Forward.  The state lies in registers over 2^eh and enters as that; R and U are over 2^er.  Both stay while the largest
+// entries (of U its bound) are between 2^-2 and 2^13 (2^-3 and 2^4) of them.  That is known to all waves only behind the
+// barrier that hands the state over: where it does not hold any more, all is scaled anew and handed over again (a few
+// times at a sequence's start).
 
 // What a launch of the forward does: the chunks c0 .. c1 - 1 of all states, from H0 to HT, in its first `scans`
 // workgroups, and T and P of the chunks c1 .. c2 - 1, which the next launch reads, in the others.
@@ -623,19 +646,20 @@ __global__ void __launch_bounds__(256, 2)
   h8_t kf[KB];
   f4_t vf[VT], ge, gl, be;
   float g1, gc;
-  int ek, eb, ep, eh = 0;
-  auto take1 = [&]() {
+  int ek, eb, ep, eq, eh = 0, er = 0;
+  auto take_keys = [&](auto far) {
+    rows_to_h8<decltype(far)::value>(nk, ek, kf);
 #pragma unroll
-    for (int i = 0; i < KB; ++i) {
-      kf[i] = bf16_to_h8(nk[i]);
-      pin8(kf[i]);
-    }
+    for (int i = 0; i < KB; ++i) pin8(kf[i]);
+  };
+  auto take1 = [&](auto far) {
     tv.put(nv);
     gs.at[lane] = ng;
+    ek = Gates::top(ng, 0); eb = Gates::top(ng, 1); ep = Gates::top(ng, 2); eq = Gates::top(ng, 3);
+    take_keys(far);
 #pragma unroll
     for (int t = 0; t < VT; ++t) vf[t] = tv.get(t);
     ge = gs.four(0); gl = gs.four(1); be = gs.four(2); g1 = gs.one(0); gc = gs.last();
-    ek = gs.k_top(); eb = gs.beta_top(); ep = gs.p_top();
   };
   auto put_state = [&]() {
     if (S::on(wv))
@@ -653,7 +677,7 @@ __global__ void __launch_bounds__(256, 2)
     fetch1(p.c0);
     fetch2(p.c0);
     if (Y) fetch3(p.c0);
-    take1();
+    take1(std::false_type());
   }
   auto get_state = [&](h8_t(&hh)[VT][KB], h8_t(&hl)[VT][KB]) {
 #pragma unroll
@@ -665,18 +689,16 @@ __global__ void __launch_bounds__(256, 2)
         hl[t][i] = ld8(Hl + o);
       }
   };
-  // R is no larger than sqrt(K) 2^er, and U not by much more while the rule does not expand.  The state counts as no
-  // smaller than 2^-24 of that, of which nothing would be left beside it.
-  auto scale_for = [&](int et, int ev, int &er) {
-    er = exponent_in_range(eb + max(ev, ek + et));
-    return max(exponent_in_range(et), er - 24);
-  };
+  // For R, which is no larger than sqrt(K) times this (and U not by much more while the rule does not expand)
+  auto scale_of_u = [&](int et, int ev) { return exponent_in_range(eb + max(ev, ek + et)); };
+  // The state counts as no smaller than 2^-24 of that, of which nothing would be left beside it.
+  auto scale_of_state = [&](int et, int tu) { return max(exponent_in_range(et), tu - 24); };
   // The exponents of the largest finite |H| and |v|
   auto measure = [&](int &et, int &ev) {
-    finite_tops(red + 16, H, vf, wv);
+    finite_tops(red + 4, H, vf, wv);
     lds_barrier();
-    et = eh + exponent_of(*(const u4_t *)(red + 16));
-    ev = exponent_of(*(const u4_t *)(red + 20));
+    et = eh + exponent_of(*(const u4_t *)(red + 4));
+    ev = exponent_of(*(const u4_t *)(red + 8));
   };
   auto rescale = [&](int to) {
 #pragma unroll
@@ -688,17 +710,22 @@ __global__ void __launch_bounds__(256, 2)
     eh = to;
   };
   if (p.c0 < p.c1) {
-    int et, ev, er;
+    int et, ev;
     measure(et, ev);
-    rescale(scale_for(et, ev, er));
+    er = scale_of_u(et, ev);
+    rescale(scale_of_state(et, er));
   }
   const int w = place(wv);
-  for (int ch = p.c0; ch < p.c1; ++ch) {
-    const int next = min(ch + 1, p.c1 - 1);
+  auto is_far = [&]() { return far_key(ek) || (Y && far_query(eq)); };
+  // the chunks from ch on; without FAR up to one whose keys or queries are far from one.  Returns the next chunk.
+  auto rounds = [&](auto far, int ch) __attribute__((always_inline)) {
+   constexpr bool FAR = decltype(far)::value;
+   while (ch < p.c1) {
+    const int next = min(ch + 1, p.c1 - 1), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
     put_state();
 #pragma unroll
     for (int i = 0; i < KB; ++i) *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
-    top_of_rows(red, H, vf, wv);
+    top_of_wave(red, H, vf, wv);
     lds_barrier();  // the state is there, and k of the chunk before has been read
     // R = beta (v - e^G K H): D[step][column]
     const uint32_t tops = top_of_all(red);
@@ -718,18 +745,20 @@ __global__ void __launch_bounds__(256, 2)
     get_state(hh, hl);
     fetch1(next);
     keys_with_state();
-    int et = eh + top_exponent(tops >> 16), ev = top_exponent(tops), er;
-    int want = scale_for(et, ev, er);
-    if (not_finite(tops) || want < eh - 2 || want > eh + 13) {  // (the same in all waves)
+    f4_t gh = two_to(eh + kx) * ge, br = two_to(-er) * be;
+    int et = eh + top_exponent(tops >> 16), ev = top_exponent(tops), tu = scale_of_u(et, ev);
+    int want = scale_of_state(et, tu);
+    if (not_finite(tops) | (want < eh - 2) | (want > eh + 13) | (tu < er - 3) | (tu > er + 4)) {  // (the same in all waves)
       measure(et, ev);
-      want = scale_for(et, ev, er);
-      rescale(want);
+      er = scale_of_u(et, ev);
+      rescale(scale_of_state(et, er));
       put_state();
       lds_barrier();
       get_state(hh, hl);
       keys_with_state();
+      gh = two_to(eh + kx) * ge;
+      br = two_to(-er) * be;
     }
-    const f4_t gh = pow2i(eh) * ge, br = pow2i(-er) * be;
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       const Pair4 s = split4(br * (vf[t] - gh * (x[t] + xl[t])));
@@ -782,7 +811,7 @@ __global__ void __launch_bounds__(256, 2)
     lds_barrier();
     // H = e^{G_C} H + K^T W: D[row][column];  y = e^G (Q H)^T + (P U)^T
     h8_t wh[VTW][2], wl[VTW][2], uf[VT][2], us;
-    const float gy = pow2i(eh) * g1, rp = pow2i(er + ep), rus = pow2i(er - eh);
+    const float gy = two_to(eh + qx) * g1, rp = two_to(er + ep), rus = two_to(er + kx - eh);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -792,14 +821,18 @@ __global__ void __launch_bounds__(256, 2)
         wl[j][kb] = ld8(Wl + o);
       }
     if (Y) {
+      h8_t qf[KB];
+      rows_to_h8<FAR>(nq, eq, qf);
 #pragma unroll
-      for (int i = 0; i < KB; ++i) {
-        const h8_t qf = bf16_to_h8(nq[i]);
+      for (int i = 0; i < KB; ++i)
 #pragma unroll
-        for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf, y[t]);
-      }
+        for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf[i], y[t]);
     }
-    f4_t kw[KTW][VTW];
+    f4_t kw[KTW][VTW], hg[KTW][VTW];
+#pragma unroll
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j) hg[i][j] = gc * H[i][j];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -814,7 +847,7 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int j = 0; j < VTW; ++j) {
         settle(kw[i][j]);
-        H[i][j] = gc * H[i][j] + rus * kw[i][j];
+        H[i][j] = fma4(rus, kw[i][j], hg[i][j]);
       }
     if (Y) {
 #pragma unroll
@@ -836,7 +869,7 @@ __global__ void __launch_bounds__(256, 2)
       }
     }
     if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
-    take1();
+    take1(far);
     if (Y) {
       const auto o = in.o.at(ch);
 #pragma unroll
@@ -853,6 +886,16 @@ __global__ void __launch_bounds__(256, 2)
       __builtin_amdgcn_raw_buffer_store_b32(lane ? er : eh, __builtin_amdgcn_make_buffer_rsrc(exps + (at * (a.V / VB) + part) * 2,
                                             0, 8, 0x00027000), 4 * (int)threadIdx.x, 0, 0);
     }
+    ++ch;
+    if (!FAR && is_far()) break;
+   }
+   return ch;
+  };
+  int ch = p.c0;
+  if (ch < p.c1 && !is_far()) ch = rounds(std::false_type(), ch);
+  if (ch < p.c1) {
+    take_keys(std::true_type());
+    rounds(std::true_type(), ch);
   }
   rescale(0);
   if (p.HT && S::on(wv))
@@ -865,11 +908,10 @@ __global__ void __launch_bounds__(256, 2)
           p.HT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] = H[i][j][x];
 }
 
-// Backward, chunks in reverse order.  As in the forward dH lies in registers over 2^ed and enters as that, dy over 2^ey,
-// from the largest ones of the workgroup's columns; dU and Z are over 2^ez, from a bound of the terms of dU (Z is not
-// much larger while the rule does not expand).  8 x 4096 steps, 16 heads of 64 x 64: 235 us, 3.7 a chunk (3.5 TB/s).
+// Backward, chunks in reverse order.  As in the forward dH lies in registers over 2^ed and enters as that, dy over 2^ey, dU
+// and Z over 2^ez.  8 x 4096 steps, 16 heads of 64 x 64: 235 us, 3.7 a chunk (3.5 TB/s).
 template <int K, int VB>
-constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 7 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 24 * 4; }
+constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 7 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 12 * 4; }
 
 template <int K, int VB>
 __global__ void __launch_bounds__(256, 2)
@@ -934,27 +976,30 @@ __global__ void __launch_bounds__(256, 2)
   h8_t kf[KB], qf[KB];
   f4_t yf[VT], ge, gl, be;
   float b1, gc, om;
-  int ek, eb, ep, eq, ed = 0, ey = 0;
-  auto take1 = [&]() {
-    ty.put(ny);
-    gs.at[lane] = ng;
+  int ek, eb, ep, eq, ed = 0, ey = 0, ez = 0;
+  auto take_rows = [&](auto far) {
+    rows_to_h8<decltype(far)::value>(nk, ek, kf);
+    rows_to_h8<decltype(far)::value>(nq, eq, qf);
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
-      kf[i] = bf16_to_h8(nk[i]);
-      qf[i] = bf16_to_h8(nq[i]);
       pin8(kf[i]);
       pin8(qf[i]);
     }
+  };
+  auto take1 = [&](auto far) {
+    ty.put(ny);
+    gs.at[lane] = ng;
+    ek = Gates::top(ng, 0); eb = Gates::top(ng, 1); ep = Gates::top(ng, 2); eq = Gates::top(ng, 3);
+    take_rows(far);
 #pragma unroll
     for (int t = 0; t < VT; ++t) yf[t] = ty.get(t);
     ge = gs.four(0); gl = gs.four(1); be = gs.four(2); b1 = gs.one(2);
     om = gate_unit(gs.first());
     gc = om * gs.last();
-    ek = gs.k_top(); eb = gs.beta_top(); ep = gs.p_top(); eq = gs.q_top();
   };
   const int w = place(wv);
   auto put_in = [&]() {
-    const float sy = pow2i(-ey);
+    const float sy = two_to(-ey);
     if (S::on(wv))
 #pragma unroll
       for (int i = 0; i < KTW; ++i)
@@ -975,17 +1020,16 @@ __global__ void __launch_bounds__(256, 2)
       *(u2_t *)&Wl[o] = x.lo;
     }
   };
-  // From the exponents of the largest |dH| and |dy|, that of dU, and that to scale dH with: dH counts as no smaller
-  // than 2^-24 of what the chunk adds to it.
-  auto scale_for = [&](int td, int ty, int &ez) {
-    ez = exponent_in_range(max(td + ek, ty + ep));
-    return max(exponent_in_range(td), exponent_in_range(max(ty + eq, ez + eb + ek)) - 24);
+  // For dU, from the exponents of the largest |dH| and |dy|; dH counts as no smaller than 2^-24 of what a chunk adds to it
+  auto scale_of_z = [&](int td, int ty) { return exponent_in_range(max(td + ek, ty + ep)); };
+  auto scale_of_dh = [&](int td, int ty, int tz) {
+    return max(exponent_in_range(td), exponent_in_range(max(ty + eq, tz + eb + ek)) - 24);
   };
   auto measure = [&](int &td, int &ty) {
-    finite_tops(red + 16, D, yf, wv);
+    finite_tops(red + 4, D, yf, wv);
     lds_barrier();
-    td = ed + exponent_of(*(const u4_t *)(red + 16));
-    ty = exponent_of(*(const u4_t *)(red + 20));
+    td = ed + exponent_of(*(const u4_t *)(red + 4));
+    ty = exponent_of(*(const u4_t *)(red + 8));
   };
   auto rescale = [&](int to) {
 #pragma unroll
@@ -1000,20 +1044,25 @@ __global__ void __launch_bounds__(256, 2)
     fetch1(chunks - 1);
     fetch2(chunks - 1);
     fetch3(chunks - 1);
-    take1();
-    int td, ez;
+    take1(std::false_type());
+    int td;
     measure(td, ey);
-    rescale(scale_for(td, ey, ez));
+    ez = scale_of_z(td, ey);
+    rescale(scale_of_dh(td, ey, ez));
   }
-  for (int ch = chunks - 1; ch >= 0; --ch) {
-    const int next = max(ch - 1, 0);
+  auto is_far = [&]() { return far_key(ek) || far_query(eq); };
+  // the chunks from ch down, as in the forward
+  auto rounds = [&](auto far, int ch) __attribute__((always_inline)) {
+   constexpr bool FAR = decltype(far)::value;
+   while (ch >= 0) {
+    const int next = max(ch - 1, 0), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
     put_in();
 #pragma unroll
     for (int i = 0; i < KB; ++i) {
       *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
       *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = qf[i];
     }
-    top_of_rows(red, D, yf, wv);
+    top_of_wave(red, D, yf, wv);
     lds_barrier();  // (of the chunk before only Z may still be read)
     // dU = P^T dY + e^{G_C - G} K dH: D[step][column]
     const uint32_t tops = top_of_all(red);
@@ -1054,23 +1103,25 @@ __global__ void __launch_bounds__(256, 2)
     get_in();
     fetch1(next);
     products();
-    int td = ed + top_exponent(tops >> 16), ty_ = top_exponent(tops), ez;
-    int want = scale_for(td, ty_, ez);
-    if (not_finite(tops) || want < ed - 2 || want > ed + 13 || ty_ < ey - 2 || ty_ > ey + 13) {  // (the same in all waves)
-      measure(td, ty_);
-      want = scale_for(td, ty_, ez);
-      rescale(want);
-      ey = ty_;
+    f4_t glz = two_to(ed + kx - ez) * gl;
+    float pz = two_to(ey + ep - ez);
+    int td = ed + top_exponent(tops >> 16), ty_ = top_exponent(tops), tz = scale_of_z(td, ty_);
+    int want = scale_of_dh(td, ty_, tz);
+    if (not_finite(tops) | (want < ed - 2) | (want > ed + 13) | (ty_ < ey - 2) | (ty_ > ey + 13) | (tz < ez - 3) |
+        (tz > ez + 4)) {  // (the same in all waves)
+      measure(td, ey);
+      ez = scale_of_z(td, ey);
+      rescale(scale_of_dh(td, ey, ez));
       put_in();
       lds_barrier();
       get_in();
       products();
+      glz = two_to(ed + kx - ez) * gl;
+      pz = two_to(ey + ep - ez);
     }
     hold();
     fetch2(next);
     hold();
-    const f4_t glz = pow2i(ed - ez) * gl;
-    const float pz = pow2i(ey + ep - ez);
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       settle(u[t]);
@@ -1128,7 +1179,7 @@ __global__ void __launch_bounds__(256, 2)
       xl[t] = mfma_k32(Tf[3], uh[t][0], xl[t]);
       xl[t] = mfma_k32(Tf[2], uo[t][0], xl[t]);
     }
-    const f4_t bg = -pow2i(-eb) * (be * ge);
+    const f4_t bg = -two_to(-eb) * (be * ge);
 #pragma unroll
     for (int t = 0; t < VT; ++t) {
       settle(x[t]);
@@ -1164,7 +1215,7 @@ __global__ void __launch_bounds__(256, 2)
     hold();
 #pragma unroll
     for (int t = 0; t < VT; ++t) settle(z[t]);
-    const float backq = om * pow2i(ey - ed), backk = om * pow2i(ez + eb - ed);
+    const float backq = om * two_to(ey + qx - ed), backk = om * two_to(ez + eb + kx - ed);
 #pragma unroll
     for (int i = 0; i < KTW; ++i)
 #pragma unroll
@@ -1186,10 +1237,10 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
       for (int j = 0; j < VTW; ++j) {
         settle(acc[i][j]);
-        D[i][j] += backk * acc[i][j];
+        D[i][j] = fma4(backk, acc[i][j], D[i][j]);
       }
-    const float bz = b1 * pow2i(ez);
-    take1();
+    const float bz = b1 * two_to(ez);
+    take1(far);
     const size_t at = (size_t)unit * chunks + ch;
     const auto o = in.o.at(ch);
 #pragma unroll
@@ -1206,6 +1257,16 @@ __global__ void __launch_bounds__(256, 2)
     // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
     __builtin_amdgcn_raw_buffer_store_b128(u4_t{(uint32_t)ed, (uint32_t)ez, (uint32_t)ey, 0u}, __builtin_amdgcn_make_buffer_rsrc(
                                            exps + at * (a.V / VB) + part, 0, 16, 0x00027000), 16 * (int)threadIdx.x, 0, 0);
+    --ch;
+    if (!FAR && is_far()) break;
+   }
+   return ch;
+  };
+  int ch = chunks - 1;
+  if (ch >= 0 && !is_far()) ch = rounds(std::false_type(), ch);
+  if (ch >= 0) {
+    take_rows(std::true_type());
+    rounds(std::true_type(), ch);
   }
   rescale(0);
   if (a.dH0 && S::on(wv))
@@ -1233,17 +1294,6 @@ __device__ __forceinline__ float dot8(h8_t a, h8_t b, float c) {
     c = __builtin_amdgcn_fdot2(h2_t{a[i], a[i + 1]}, h2_t{b[i], b[i + 1]}, c, false);
   return c;
 }
-// eight bf16 values times s, as fp16
-__device__ __forceinline__ h8_t bf16_to_h8(u4_t w, float s) {
-  u4_t r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t x = w[i];
-    r[i] = pack2_h(s * __builtin_bit_cast(float, x << 16), s * __builtin_bit_cast(float, x & 0xFFFF0000u));
-  }
-  return __builtin_bit_cast(h8_t, r);
-}
-
 template <int K, int V32>
 __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
     delta_half_grad_kernel(DeltaArgs a, int chunks, int vbs, const float *__restrict__ gates,
@@ -1284,19 +1334,25 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   const int et = row_top(el), eY = __builtin_amdgcn_readlane(row_top(ey), 0);
   const int eh = __builtin_amdgcn_readlane(et, 0), eu = __builtin_amdgcn_readlane(et, 16);
   const int eD = __builtin_amdgcn_readlane(et, 32), eZ = __builtin_amdgcn_readlane(et, 48);
-  const int fl = __builtin_bit_cast(unsigned short, (half_t)pow2i(el - et));
+  const int fl = __builtin_bit_cast(unsigned short, (half_t)two_to(el - et));
   auto own_factor = [&](int kind, int vb) {
     const half_t f = __builtin_bit_cast(half_t, (unsigned short)__shfl(fl, 16 * kind + (vbs == 32 ? vb : 2 * vb + (g4 >> 1)), 64));
     return h8_t{f, f, f, f, f, f, f, f};
   };
   const int *gt_tops = (const int *)gates + at * kGates + kTops;
-  const int eb = gt_tops[1];
-  const float sy = pow2i(-eY), sb = pow2i(-eb);
+  const int eb = gt_tops[1], ek = far_key(gt_tops[0]) ? gt_tops[0] : 0, eq = far_query(gt_tops[3]) ? gt_tops[3] : 0;
+  const float sy = two_to(-eY), sb = two_to(-eb);
 
+  {
+    h8_t x[KB];
+    if (ek) rows_to_h8<true>(kr, ek, x);
+    else rows_to_h8<false>(kr, 0, x);
 #pragma unroll
-  for (int e = 0; e < KB; ++e) {
-    *(h8_t *)&ks[i * LK + 32 * e + 8 * g4] = bf16_to_h8(kr[e]);
-    *(h8_t *)&qs[i * LK + 32 * e + 8 * g4] = bf16_to_h8(qr[e]);
+    for (int e = 0; e < KB; ++e) *(h8_t *)&ks[i * LK + 32 * e + 8 * g4] = x[e];
+    if (eq) rows_to_h8<true>(qr, eq, x);
+    else rows_to_h8<false>(qr, 0, x);
+#pragma unroll
+    for (int e = 0; e < KB; ++e) *(h8_t *)&qs[i * LK + 32 * e + 8 * g4] = x[e];
   }
   for (int x = threadIdx.x; x < kTops; x += 256) {
     const float g = gates[at * kGates + x];
@@ -1384,7 +1440,7 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   }
   __syncthreads();
   const int x1 = exponent_of(*(const f4_t *)red), x2 = exponent_of(*(const f4_t *)(red + 4));
-  const float ss1 = pow2i(-x1), ss2 = pow2i(-x2), bt = ge[4 * C + i], gt = ge[C + i];
+  const float ss1 = two_to(-x1), ss2 = two_to(-x2), bt = ge[4 * C + i], gt = ge[C + i];
   const float om = gate_unit(ge[2 * C]), gm = om * ge[i];
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt) {  // (the last tile of an even wave's pair is zero)
@@ -1410,9 +1466,10 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   __syncthreads();
   const bool heads = a.N != a.Nqk;
   // every product with the powers of two that its factors came without
-  const float cq = gm * pow2i(eh + eY), ca = -gm * pow2i(eh + eZ), ck = gt * pow2i(eu + eD);
-  const float c1 = pow2i(x1 + eu + eY), c2 = pow2i(x2 + eu + eZ), cb = pow2i(x2 + eu + eZ + eb);
-  float dG = 0.f, kb1 = 0.f, tail = 0.f;
+  const float cq = gm * two_to(eh + eY), ca = -gm * two_to(eh + eZ), ck = gt * two_to(eu + eD);
+  const float c1k = two_to(x1 + eu + eY + ek), c1q = two_to(x1 + eu + eY + eq), c2 = two_to(x2 + eu + eZ + ek);
+  const float cb = two_to(x2 + eu + eZ + eb + ek);
+  float dGq = 0.f, dGk = 0.f, kb1 = 0.f, tail = 0.f;
   h8_t row1[2], row2[2], col1[2], colb[2];
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
@@ -1441,15 +1498,15 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
     f4_t o;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float qx = (float)qv[r], kx = (float)kv[r];
-      x[r] = fmaf(c1, x[r], cq * dq[kt][r]);
+      const float q_ = (float)qv[r], k_ = (float)kv[r];
+      x[r] = fmaf(c1k, x[r], cq * dq[kt][r]);
       y[r] = fmaf(c2, y[r], ca * as[kt][r]);
-      w[r] = fmaf(c1, w[r], fmaf(cb, wb[r], ck * kd[r]));
+      w[r] = fmaf(c1q, w[r], fmaf(cb, wb[r], ck * kd[r]));
       o[r] = fmaf(bt, y[r], w[r]);
-      dG = fmaf(qx, x[r], dG);
-      dG = fmaf(kx, fmaf(bt, y[r], -w[r]), dG);
-      kb1 = fmaf(kx, y[r], kb1);
-      tail = fmaf(ck * kx, kd[r], tail);
+      dGq = fmaf(q_, x[r], dGq);
+      dGk = fmaf(k_, fmaf(bt, y[r], -w[r]), dGk);
+      kb1 = fmaf(k_, y[r], kb1);
+      tail = fmaf(ck * k_, kd[r], tail);
     }
     if (own < a.T) {
       const size_t m = ((size_t)b * a.T + own) * (heads ? a.N : a.Nqk) * K + (size_t)(heads ? n : nq) * K + 16 * kt + 4 * g4;
@@ -1462,6 +1519,10 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
       }
     }
   }
+  const float k1 = two_to(ek);
+  float dG = fmaf(two_to(eq), dGq, k1 * dGk);
+  kb1 *= k1;
+  tail *= k1;
   dG += __shfl_xor(dG, 16, 64);
   dG += __shfl_xor(dG, 32, 64);
   kb1 += __shfl_xor(kb1, 16, 64);
@@ -1471,12 +1532,12 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   if (lane == 0) red[12 + wv] = tail;
   if (g4 == 0) red[16 + i] = dG;
   if (g4 == 0 && own < a.T)
-    ((__hip_bfloat16 *)a.dbeta)[((size_t)b * a.T + own) * a.N + n] = __float2bfloat16(pow2i(eZ) * zv + kb1);
+    ((__hip_bfloat16 *)a.dbeta)[((size_t)b * a.T + own) * a.N + n] = __float2bfloat16(two_to(eZ) * zv + kb1);
   __syncthreads();
   if (wv == 0) {  // sums over the steps behind, in 64 bits; <H_C, dH> at the last one
     double s = (double)red[16 + lane];
     if (lane == C - 1)
-      for (int w = 0; w < 4; ++w) s += (double)(om * ge[C - 1]) * pow2i(eh + eD) * red[8 + w] + red[12 + w];
+      for (int w = 0; w < 4; ++w) s += (double)(om * ge[C - 1]) * two_to(eh + eD) * red[8 + w] + red[12 + w];
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
       const double o = __shfl_down(s, m, 64);

@@ -53,10 +53,20 @@ def test_gradients_of_any_size(io, B, T, N, K, V):
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("B,T,N,K,V", SIZES)
-def test_large_queries(io, B, T, N, K, V):
-    """(Entries of q far below its largest are not exact as fp16, so the bits differ.)"""
-    s = times(dr.rule_inputs(65, B, T, N, K, V, io=io), q=13, dHT=13)
-    small.check(small.run(s, io), dr.rule(s), (io, B, T, N, K, V))
+@pytest.mark.parametrize("e", [-60, -13, 13, 60])
+def test_queries_of_any_size(io, B, T, N, K, V, e):
+    """(Entries of q far below its largest are not always exact as fp16, so the bits may differ.)"""
+    s = times(dr.rule_inputs(65, B, T, N, K, V, io=io), q=e, dHT=e)
+    small.check(small.run(s, io), dr.rule(s), (io, B, T, N, K, V, e))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,N,K,V", SIZES)
+@pytest.mark.parametrize("e", [-20, -10, 10, 20])
+def test_keys_of_any_size(io, B, T, N, K, V, e):
+    """Betas that make up for it: u is 2^-2e, the state 2^-e of what it is with unit keys."""
+    s = times(dr.rule_inputs(68, B, T, N, K, V, io=io), k=e, beta=-2 * e, H0=-e, dHT=e)
+    small.check(small.run(s, io), dr.rule(s), (io, B, T, N, K, V, e))
 
 
 @pytest.mark.parametrize("T", [13, 65, 130])
