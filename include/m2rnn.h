@@ -323,7 +323,7 @@ m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t group
  *   dH0 [B,N,K,V] fp32, or NULL; may be dHT (segments of a sequence, from the last to the first)
  *   H0 is read only where ckpt is NULL (a forward that carried its state in place has overwritten it).
  *   workspace: m2rnn_delta_workspace_bytes(desc, 0 forward | 1 backward with ckpt | 2 without).
- *   N V and Nqk K below 2^23; B N (T / 32 + 1) below 2^24.
+ *   N V and Nqk K below 2^23; B N at most 2^20 - 8, B N (T / 32 + 1) below 2^24.
  * Numbers: fp32 io is computed in fp32 throughout (and bf16 io with K = 16 or V = 16).  bf16 io feeds fp16 matrix-core
  * operands: magnitudes of q, k, v, the state and products of two keys or of a query and a key must stay below
  * 2*10^4; the states and dH0 are as good as fp32 with operands of 22 bits, other results carry the 11 bits that

@@ -15,9 +15,10 @@ m2rnn_status check(const m2rnn_desc *d) {
   const auto dim = [](int x) { return x == 16 || x == 32 || x == 64 || x == 128; };
   if (!dim(d->K) || !(dim(d->V) || d->V == 256) || d->flags != 0) return M2RNN_ERR_SHAPE;
   if ((double)d->B * (d->T > 0 ? d->T : 1) * d->N * d->K * d->V > 1e15) return M2RNN_ERR_SHAPE;
-  // (units times parts or chunks are workgroups of 256 threads, of which a launch has fewer than 2^32)
+  // (units times parts or chunks are workgroups of 256 threads, of which a launch has fewer than 2^32; for the parts
+  // delta_grid counts units in eights)
   const double units = (double)d->B * d->N, most = (1 << 24) - 1;
-  if (units * 16 > most || units * (d->T / 32 + 1) > most) return M2RNN_ERR_SHAPE;
+  if (units > (1 << 20) - 8 || units * (d->T / 32 + 1) > most) return M2RNN_ERR_SHAPE;
   // (a chunk's rows are reached by 31-bit byte offsets)
   if ((double)d->N * d->V >= (1 << 23) || (double)d->Nqk * d->K >= (1 << 23)) return M2RNN_ERR_SHAPE;
   if (d->chunk != 0) return M2RNN_ERR_CHUNK;

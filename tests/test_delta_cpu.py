@@ -170,3 +170,14 @@ def test_a_count_beyond_32_bits_is_not_cut_to_one_that_fits():
     for groups, mode in (((1 << 32) + 2, 0), (2, 1 << 32), (-(1 << 32) + 2, 0)):
         with pytest.raises(ValueError, match="too large"):
             mb.m2rnn_group_norm_fwd(x, None, cpu(16), None, groups, 1e-5, mode, x)
+
+
+@pytest.mark.parametrize("V", [16, 32, 256])
+@pytest.mark.parametrize("io", [mb.M2RNN_F32, mb.M2RNN_BF16])
+def test_as_many_states_as_a_launch_can_have(V, io):
+    """16 workgroups of 256 threads for each eight states: 2^32 threads from 2^20 - 7 states on."""
+    most = (1 << 20) - 8
+    assert mb.m2rnn_delta_workspace_bytes(desc(B=most, N=1, K=16, V=V, T=1, io=io), 0) > 0
+    for B in (most + 1, most + 7, most + 8):
+        d = desc(B=B, N=1, K=16, V=V, T=1, io=io)
+        assert mb.m2rnn_delta_workspace_bytes(d, 0) == 0 and fwd(d) == 2 and bwd(d) == 2
