@@ -141,7 +141,8 @@ def _call():
                                % (built_for, torch.__version__, again))
         address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         module.init(address(L.m2rnn_fwd_opt), address(L.m2rnn_bwd_opt))
-        module.init_layer(address(L.m2rnn_delta_fwd), address(L.m2rnn_delta_bwd), address(L.m2rnn_group_norm_fwd),
+        module.init_layer(address(L.m2rnn_delta_fwd), address(L.m2rnn_delta_bwd), address(L.m2rnn_delta_ckpt_bytes),
+                          address(L.m2rnn_group_norm_fwd), address(L.m2rnn_group_norm_bwd),
                           address(L.m2rnn_conv_silu_window_fwd))
         _call_module = module
     return _call_module
@@ -322,11 +323,9 @@ def m2rnn_group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream=None, check=
 
 def m2rnn_group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, stream=None, check=True):
     """Gradients of m2rnn_group_norm_fwd: dx, da (with a), dw and db [D] fp32 (None: not wanted; without both no
-    workspace is needed)."""
-    B, T, D = x.shape
-    rc = lib().m2rnn_group_norm_bwd(B, T, D, groups, _io_code(x), mode, _ptr(x), _ptr(a), _ptr(w), _ptr(b),
-                                    float(eps), _ptr(dout), _ptr(dx), _ptr(da), _ptr(dw), _ptr(db),
-                                    _ptr(workspace), _nbytes(workspace), stream or 0)
+    workspace is needed).  Tensors are checked (ValueError)."""
+    rc = _call().group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, stream or 0,
+                                _nbytes(workspace))
     return _check(rc, "m2rnn_group_norm_bwd", check)
 
 

@@ -1,11 +1,12 @@
-// Python module _call: entry points of the C ABI called with torch tensors: those of Scan and Delta, and the
-// forwards of the block's group norm and windowed convolution, which serving calls for every token.
+// Python module _call: entry points of the C ABI called with torch tensors: those of Scan and Delta, the block's
+// group norm and the windowed convolution.
 //
 // A decode step is one kernel of some 4 us, and handing its sixteen arguments over through ctypes took
 // 2.5 us of host time (on a slower host 6), beside a launch of 3.5.  Here the addresses are taken from the
 // tensors directly and the options are put on the stack: 0.2 us (0.4).  The library is the one
 // that ctypes has loaded; its entry points come in as addresses.
 #include <Python.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/m2rnn.h"
@@ -16,7 +17,9 @@ decltype(&m2rnn_fwd_opt) fwd_opt = nullptr;
 decltype(&m2rnn_bwd_opt) bwd_opt = nullptr;
 decltype(&m2rnn_delta_fwd) delta_fwd = nullptr;
 decltype(&m2rnn_delta_bwd) delta_bwd = nullptr;
+decltype(&m2rnn_delta_ckpt_bytes) delta_ckpt_bytes = nullptr;
 decltype(&m2rnn_group_norm_fwd) group_norm_fwd = nullptr;
+decltype(&m2rnn_group_norm_bwd) group_norm_bwd = nullptr;
 decltype(&m2rnn_conv_silu_window_fwd) window_fwd = nullptr;
 
 // None -> NULL, an int as it is, a tensor -> its address, anything else -> what its data_ptr() says (a
@@ -125,16 +128,19 @@ PyObject *bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 PyObject *init_layer(PyObject *, PyObject *const *args, Py_ssize_t n) {
-  void *p[4];
-  if (!arity(n, 4) || !addresses(args, p)) return nullptr;
-  if (!p[0] || !p[1] || !p[2] || !p[3]) {
-    PyErr_SetString(PyExc_ValueError, "an entry point is NULL");
-    return nullptr;
-  }
+  void *p[6];
+  if (!arity(n, 6) || !addresses(args, p)) return nullptr;
+  for (const void *entry : p)
+    if (!entry) {
+      PyErr_SetString(PyExc_ValueError, "an entry point is NULL");
+      return nullptr;
+    }
   delta_fwd = (decltype(delta_fwd))p[0];
   delta_bwd = (decltype(delta_bwd))p[1];
-  group_norm_fwd = (decltype(group_norm_fwd))p[2];
-  window_fwd = (decltype(window_fwd))p[3];
+  delta_ckpt_bytes = (decltype(delta_ckpt_bytes))p[2];
+  group_norm_fwd = (decltype(group_norm_fwd))p[3];
+  group_norm_bwd = (decltype(group_norm_bwd))p[4];
+  window_fwd = (decltype(window_fwd))p[5];
   Py_RETURN_NONE;
 }
 
@@ -161,6 +167,19 @@ bool operand(PyObject *o, const char *name, at::ScalarType type, int64_t count, 
   }
   return true;
 }
+// Room of at least `bytes` bytes, as a tensor of any type, an address or None.
+bool room(PyObject *o, const char *name, size_t bytes, long device, void *&p) {
+  if (THPVariable_Check(o)) {
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!operand(o, name, t.scalar_type(), t.numel(), device, p)) return false;
+    if (t.nbytes() < bytes) {
+      PyErr_Format(PyExc_ValueError, "%s has fewer bytes than the call takes", name);
+      return false;
+    }
+    return true;
+  }
+  return address(o, p);
+}
 at::ScalarType io_type(int32_t io) { return io == M2RNN_BF16 ? at::kBFloat16 : at::kFloat; }
 
 struct DeltaSizes {
@@ -177,7 +196,7 @@ struct DeltaSizes {
 // delta_fwd(desc, q, k, v, g, beta, H0, y, HT, ckpt, workspace, stream, bytes, device) -> status
 PyObject *call_delta_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (!ready((const void *)delta_fwd) || !arity(n, 14)) return nullptr;
-  void *d, *q, *k, *v, *g, *beta, *H0, *y, *HT, *rest[3];
+  void *d, *q, *k, *v, *g, *beta, *H0, *y, *HT, *ckpt, *ws, *stream;
   const size_t bytes = PyLong_AsSize_t(args[12]);
   const long dev = PyLong_AsLong(args[13]);
   if (PyErr_Occurred() || !address(args[0], d)) return nullptr;
@@ -188,12 +207,13 @@ PyObject *call_delta_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
       !operand(args[3], "v", io, z.v, dev, v) || !operand(args[4], "g", f, z.gates, dev, g) ||
       !operand(args[5], "beta", f, z.gates, dev, beta) || !operand(args[6], "H0", f, z.state, dev, H0) ||
       !operand(args[7], "y", io, z.v, dev, y) || !operand(args[8], "HT", f, z.state, dev, HT) ||
-      !addresses(args + 9, rest))
+      !room(args[9], "ckpt", args[9] == Py_None ? 0 : delta_ckpt_bytes(desc), dev, ckpt) ||
+      !room(args[10], "workspace", bytes, dev, ws) || !address(args[11], stream))
     return nullptr;
   m2rnn_status st;
   Py_BEGIN_ALLOW_THREADS
-  st = delta_fwd(desc, q, k, v, (const float *)g, (const float *)beta, (const float *)H0, y, (float *)HT, rest[0],
-                 rest[1], bytes, rest[2]);
+  st = delta_fwd(desc, q, k, v, (const float *)g, (const float *)beta, (const float *)H0, y, (float *)HT, ckpt,
+                 ws, bytes, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
@@ -202,7 +222,7 @@ PyObject *call_delta_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
 // -> status
 PyObject *call_delta_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (!ready((const void *)delta_bwd) || !arity(n, 20)) return nullptr;
-  void *d, *q, *k, *v, *g, *beta, *H0, *ckpt, *dy, *dHT, *out[8];
+  void *d, *q, *k, *v, *g, *beta, *H0, *ckpt, *dy, *dHT, *dq, *dk, *dv, *dg, *dbeta, *dH0, *ws, *stream;
   const size_t bytes = PyLong_AsSize_t(args[18]);
   const long dev = PyLong_AsLong(args[19]);
   if (PyErr_Occurred() || !address(args[0], d)) return nullptr;
@@ -212,18 +232,23 @@ PyObject *call_delta_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (!operand(args[1], "q", io, z.qk, dev, q) || !operand(args[2], "k", io, z.qk, dev, k) ||
       !operand(args[3], "v", io, z.v, dev, v) || !operand(args[4], "g", f, z.gates, dev, g) ||
       !operand(args[5], "beta", f, z.gates, dev, beta) || !operand(args[6], "H0", f, z.state, dev, H0) ||
-      !address(args[7], ckpt) || !operand(args[8], "dy", io, z.v, dev, dy) ||
-      !operand(args[9], "dHT", f, z.state, dev, dHT) || !addresses(args + 10, out))
+      !room(args[7], "ckpt", args[7] == Py_None ? 0 : delta_ckpt_bytes(desc), dev, ckpt) ||
+      !operand(args[8], "dy", io, z.v, dev, dy) || !operand(args[9], "dHT", f, z.state, dev, dHT) ||
+      !operand(args[10], "dq", io, z.qk, dev, dq) || !operand(args[11], "dk", io, z.qk, dev, dk) ||
+      !operand(args[12], "dv", io, z.v, dev, dv) || !operand(args[13], "dg", io, z.gates, dev, dg) ||
+      !operand(args[14], "dbeta", io, z.gates, dev, dbeta) || !operand(args[15], "dH0", f, z.state, dev, dH0) ||
+      !room(args[16], "workspace", bytes, dev, ws) || !address(args[17], stream))
     return nullptr;
   m2rnn_status st;
   Py_BEGIN_ALLOW_THREADS
   st = delta_bwd(desc, q, k, v, (const float *)g, (const float *)beta, (const float *)H0, ckpt, dy, (const float *)dHT,
-                 out[0], out[1], out[2], out[3], out[4], (float *)out[5], out[6], bytes, out[7]);
+                 dq, dk, dv, dg, dbeta, (float *)dH0, ws, bytes, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
 
-// The sizes and the type of x [B,T,D]; false with a Python error set
+// The sizes and the type of x [B,T,D], and the current GPU, which all tensors have to be on (a stream belongs to it);
+// false with a Python error set
 bool shape_of(PyObject *o, int32_t (&size)[3], int32_t &io, long &device) {
   if (!THPVariable_Check(o)) {
     PyErr_SetString(PyExc_TypeError, "x: expected a tensor");
@@ -242,8 +267,24 @@ bool shape_of(PyObject *o, int32_t (&size)[3], int32_t &io, long &device) {
     size[i] = (int32_t)t.size(i);
   }
   io = t.scalar_type() == at::kBFloat16 ? M2RNN_BF16 : M2RNN_F32;
-  device = t.is_cuda() ? t.get_device() : -1;
+  device = -1;
+  try {
+    if (t.is_cuda()) device = c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index();
+  } catch (const std::exception &e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return false;
+  }
   return true;
+}
+// groups, eps and mode
+bool norm_of(PyObject *const *args, int32_t &groups, float &eps, int32_t &mode) {
+  const long g = PyLong_AsLong(args[0]), m = PyLong_AsLong(args[2]);
+  eps = (float)PyFloat_AsDouble(args[1]);
+  if (PyErr_Occurred()) return false;
+  groups = (int32_t)g;
+  mode = (int32_t)m;
+  if (groups != g || mode != m) PyErr_SetString(PyExc_ValueError, "groups or mode is too large");
+  return groups == g && mode == m;
 }
 
 // group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream) -> status
@@ -251,22 +292,45 @@ PyObject *call_group_norm_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
   int32_t s[3], io;
   long dev;
   if (!ready((const void *)group_norm_fwd) || !arity(n, 9) || !shape_of(args[0], s, io, dev)) return nullptr;
-  const long groups = PyLong_AsLong(args[4]), mode = PyLong_AsLong(args[6]);
-  const double eps = PyFloat_AsDouble(args[5]);
-  if (!PyErr_Occurred() && (groups != (int32_t)groups || mode != (int32_t)mode)) {
-    PyErr_SetString(PyExc_ValueError, "groups or mode is too large");
-    return nullptr;
-  }
+  int32_t groups, mode;
+  float eps;
   void *x, *a, *w, *b, *out, *stream;
   const int64_t all = (int64_t)s[0] * s[1] * s[2];
   const at::ScalarType t = io_type(io);
-  if (PyErr_Occurred() || !operand(args[0], "x", t, all, dev, x) || !operand(args[1], "a", t, all, dev, a) ||
+  if (!norm_of(args + 4, groups, eps, mode) || !operand(args[0], "x", t, all, dev, x) || !operand(args[1], "a", t, all, dev, a) ||
       !operand(args[2], "w", t, s[2], dev, w) || !operand(args[3], "b", t, s[2], dev, b) ||
       !operand(args[7], "out", t, all, dev, out) || !address(args[8], stream))
     return nullptr;
   m2rnn_status st;
   Py_BEGIN_ALLOW_THREADS
-  st = group_norm_fwd(s[0], s[1], s[2], (int32_t)groups, io, (int32_t)mode, x, a, w, b, (float)eps, out, stream);
+  st = group_norm_fwd(s[0], s[1], s[2], groups, io, mode, x, a, w, b, eps, out, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+
+// group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, stream, bytes) -> status
+PyObject *call_group_norm_bwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
+  int32_t s[3], io;
+  long dev;
+  if (!ready((const void *)group_norm_bwd) || !arity(n, 15) || !shape_of(args[0], s, io, dev)) return nullptr;
+  int32_t groups, mode;
+  float eps;
+  const size_t bytes = PyLong_AsSize_t(args[14]);
+  if (PyErr_Occurred()) return nullptr;
+  void *x, *a, *w, *b, *dout, *dx, *da, *dw, *db, *ws, *stream;
+  const int64_t all = (int64_t)s[0] * s[1] * s[2];
+  const at::ScalarType t = io_type(io), f = at::kFloat;
+  if (!norm_of(args + 4, groups, eps, mode) || !operand(args[0], "x", t, all, dev, x) ||
+      !operand(args[1], "a", t, all, dev, a) || !operand(args[2], "w", t, s[2], dev, w) ||
+      !operand(args[3], "b", t, s[2], dev, b) || !operand(args[7], "dout", t, all, dev, dout) ||
+      !operand(args[8], "dx", t, all, dev, dx) || !operand(args[9], "da", t, all, dev, da) ||
+      !operand(args[10], "dw", f, s[2], dev, dw) || !operand(args[11], "db", f, s[2], dev, db) ||
+      !room(args[12], "workspace", bytes, dev, ws) || !address(args[13], stream))
+    return nullptr;
+  m2rnn_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = group_norm_bwd(s[0], s[1], s[2], groups, io, mode, x, a, w, b, eps, dout, dx, da, (float *)dw, (float *)db, ws,
+                      bytes, stream);
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
@@ -294,6 +358,7 @@ PyObject *call_window_fwd(PyObject *, PyObject *const *args, Py_ssize_t n) {
 PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)(void))init, METH_FASTCALL, nullptr},
                          {"init_layer", (PyCFunction)(void (*)(void))init_layer, METH_FASTCALL, nullptr},
                          {"group_norm_fwd", (PyCFunction)(void (*)(void))call_group_norm_fwd, METH_FASTCALL, nullptr},
+                         {"group_norm_bwd", (PyCFunction)(void (*)(void))call_group_norm_bwd, METH_FASTCALL, nullptr},
                          {"window_fwd", (PyCFunction)(void (*)(void))call_window_fwd, METH_FASTCALL, nullptr},
                          {"delta_fwd", (PyCFunction)(void (*)(void))call_delta_fwd, METH_FASTCALL, nullptr},
                          {"delta_bwd", (PyCFunction)(void (*)(void))call_delta_bwd, METH_FASTCALL, nullptr},

@@ -181,3 +181,32 @@ def test_as_many_states_as_a_launch_can_have(V, io):
     for B in (most + 1, most + 7, most + 8):
         d = desc(B=B, N=1, K=16, V=V, T=1, io=io)
         assert mb.m2rnn_delta_workspace_bytes(d, 0) == 0 and fwd(d) == 2 and bwd(d) == 2
+
+
+def test_outputs_and_rooms_are_checked_as_inputs_are():
+    """A tensor in any place of a call, the others addresses: one on the host is refused by its name."""
+    d = desc()
+    io, f = "bfloat16", "float32"
+    qk, v, gates, state = (2, 70, 4, 32), (2, 70, 4, 32), (2, 70, 4), (2, 4, 32, 32)
+    grads = [("dq", qk, io), ("dk", qk, io), ("dv", v, io), ("dg", gates, io), ("dbeta", gates, io), ("dH0", state, f)]
+    backward = [("q", qk, io), ("k", qk, io), ("v", v, io), ("g", gates, f), ("beta", gates, f), ("H0", state, f),
+                ("ckpt", (1 << 20,), "uint8"), ("dy", v, io), ("dHT", state, f)] + grads + [("workspace", (1 << 20,), "uint8")]
+    forward = backward[:6] + [("y", v, io), ("HT", state, f), ("ckpt", (1 << 20,), "uint8"), ("workspace", (1 << 20,), "uint8")]
+    for call, places in ((mb._call().delta_fwd, forward), (mb._call().delta_bwd, backward)):
+        for i, (name, shape, dtype) in enumerate(places):
+            args = [A] * len(places)
+            args[i] = cpu(*shape, dtype=dtype)
+            with pytest.raises(ValueError, match="%s is not on the GPU" % name):
+                call(ctypes.addressof(d), *args, 0, 1 << 20, -1)
+
+
+def test_the_backward_of_a_norm_checks_its_tensors():
+    x, w = cpu(2, 3, 16), cpu(16)
+    with pytest.raises(ValueError, match="x is not on the GPU"):
+        mb.m2rnn_group_norm_bwd(x, None, w, None, 2, 1e-5, 0, x, cpu(2, 3, 16), None, None, None, None)
+    with pytest.raises(ValueError, match="x: expected"):
+        mb.m2rnn_group_norm_bwd(cpu(2, 16), None, w, None, 2, 1e-5, 0, x, x, None, None, None, None)
+    with pytest.raises(ValueError, match="too large"):
+        mb.m2rnn_group_norm_bwd(x, None, w, None, (1 << 32) + 2, 1e-5, 0, x, x, None, None, None, None)
+    with pytest.raises(TypeError):
+        mb.m2rnn_group_norm_bwd(A, None, w, None, 2, 1e-5, 0, x, x, None, None, None, None)
