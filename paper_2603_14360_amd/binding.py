@@ -302,10 +302,21 @@ def m2rnn_gated_rmsnorm_bwd(y, a, w, eps, s, dout, dy, da, dw, workspace, stream
     return _check(rc, "m2rnn_gated_rmsnorm_bwd", check)
 
 
+def _stream_for(x, stream):
+    """`stream`, or for None torch's current one where x is on a GPU (the calls beside Delta, which runs there)."""
+    if stream is not None:
+        return stream
+    if not getattr(x, "is_cuda", False):
+        return 0
+    import torch
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
+
+
 def m2rnn_conv_silu_window_fwd(x, w, bias, win, out, win_out, stream=None, check=True):
     """m2rnn_conv_silu_fwd that starts from the steps in win [B,3,C] (None: zeros) and hands its last three
-    on in win_out (None: not wanted; may be win).  Tensors are checked (ValueError)."""
-    rc = _call().window_fwd(x, w, bias, win, out, win_out, stream or 0)
+    on in win_out (None: not wanted; may be win).  Tensors are checked (ValueError).  stream None: torch's current
+    one, as Delta."""
+    rc = _call().window_fwd(x, w, bias, win, out, win_out, _stream_for(x, stream))
     return _check(rc, "m2rnn_conv_silu_window_fwd", check)
 
 
@@ -316,15 +327,15 @@ def m2rnn_group_norm_workspace_bytes(B, T, D):
 def m2rnn_group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream=None, check=True):
     """out = n, SiLU(n) (M2RNN_NORM_SILU) or n SiLU(a): n is x [B,T,D], each token's `groups` groups of channels
     normalised (M2RNN_NORM_CENTER: about their mean), times w [D] plus b [D] (None: 1, 0).  Tensors are
-    checked (ValueError)."""
-    rc = _call().group_norm_fwd(x, a, w, b, groups, eps, mode, out, stream or 0)
+    checked (ValueError).  stream None: torch's current one, as Delta."""
+    rc = _call().group_norm_fwd(x, a, w, b, groups, eps, mode, out, _stream_for(x, stream))
     return _check(rc, "m2rnn_group_norm_fwd", check)
 
 
 def m2rnn_group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, stream=None, check=True):
     """Gradients of m2rnn_group_norm_fwd: dx, da (with a), dw and db [D] fp32 (None: not wanted; without both no
-    workspace is needed).  Tensors are checked (ValueError)."""
-    rc = _call().group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, stream or 0,
+    workspace is needed).  Tensors are checked (ValueError).  stream None: torch's current one, as Delta."""
+    rc = _call().group_norm_bwd(x, a, w, b, groups, eps, mode, dout, dx, da, dw, db, workspace, _stream_for(x, stream),
                                 _nbytes(workspace))
     return _check(rc, "m2rnn_group_norm_bwd", check)
 

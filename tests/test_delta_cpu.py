@@ -210,3 +210,18 @@ def test_the_backward_of_a_norm_checks_its_tensors():
         mb.m2rnn_group_norm_bwd(x, None, w, None, (1 << 32) + 2, 1e-5, 0, x, x, None, None, None, None)
     with pytest.raises(TypeError):
         mb.m2rnn_group_norm_bwd(A, None, w, None, 2, 1e-5, 0, x, x, None, None, None, None)
+
+
+def test_calls_beside_delta_take_torchs_current_stream(monkeypatch):
+    """... of x's GPU, unless they are given one; 0 is the null stream."""
+    import torch
+
+    class OnGpu:
+        is_cuda = True
+
+        def get_device(self):
+            return 3
+
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 1000 + device, raising=False)
+    assert mb._stream_for(OnGpu(), None) == 1003 and mb._stream_for(OnGpu(), 0) == 0 and mb._stream_for(OnGpu(), 77) == 77
+    assert mb._stream_for(cpu(1), None) == 0 and mb._stream_for(A, None) == 0

@@ -1,5 +1,5 @@
-"""GPU: what the calls of the gated delta rule and the group norm refuse.  Nothing here is launched: outputs keep what they
-held."""
+"""GPU: what the calls of the gated delta rule and the group norm refuse (nothing is launched then: outputs keep what they
+held), and the stream that calls beside Delta run on."""
 import pytest
 
 from paper_2603_14360_amd import binding as mb
@@ -70,3 +70,34 @@ def test_tensors_of_the_backward_of_a_norm():
     torch.cuda.synchronize()
     for n in ("dx", "da", "dw", "db"):
         assert (good[n] == 7).all(), n
+
+
+def test_calls_without_a_stream_run_on_the_current_one():
+    """As Delta does: a capture holds them all, in order, and replays them on other inputs."""
+    import torch
+    B, T, G, L = 2, 9, 4, 64
+    D = G * L
+    gen = torch.Generator(device="cuda").manual_seed(82)
+    new = lambda *shape: torch.randn(shape, generator=gen, device="cuda")
+    x, cw, win, w, dout, ws = new(B, T, D), new(D, 4), new(B, 3, D), new(D), new(B, T, D), new(1 << 16)
+
+    def call():
+        u, out, dx, dw, nxt = (torch.empty_like(t) for t in (x, x, x, w, win))
+        mb.m2rnn_conv_silu_window_fwd(x, cw, None, win, u, nxt)
+        mb.m2rnn_group_norm_fwd(u, None, w, None, G, 1e-5, 0, out)
+        mb.m2rnn_group_norm_bwd(u, None, w, None, G, 1e-5, 0, dout, dx, None, dw, None, ws)
+        return u, out, dx, dw, nxt
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for _ in range(3):
+        for t in (x, win, dout):
+            t.copy_(new(*t.shape))
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
