@@ -38,7 +38,8 @@ hipError_t run_bwd(const DeltaArgs &a, hipStream_t s) { return half(a) ? delta_h
 
 size_t ckpt_bytes(const DeltaLayout &l) { return l.states + l.rows + l.exps + (l.kept ? l.gates + l.mats : 0); }
 size_t ws_bytes(const DeltaLayout &l, int bwd) {
-  const size_t fwd = l.gates + l.mats + l.carry;
+  // (a backward finds what is kept with the checkpoints there)
+  const size_t fwd = (bwd && l.kept ? 0 : l.gates + l.mats) + l.carry;
   return bwd ? fwd + l.states + l.rows + l.dexps + 2 * l.heads + (bwd >= 2 ? ckpt_bytes(l) : 0) : fwd;
 }
 bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }

@@ -613,7 +613,7 @@ Ws carve(const DeltaLayout &l, char *p, char *ckpt) {
   char *m = ckpt ? ckpt + l.states + l.rows : p;
   w.gates = (float *)m;
   w.mats = (float *)(m + l.gates);
-  p += l.gates + l.mats;
+  if (!ckpt) p += l.gates + l.mats;
   w.states = (float *)p;
   w.rows = (float *)(p += l.states);
   w.dqh = (float *)(p += l.rows);

@@ -225,3 +225,11 @@ def test_calls_beside_delta_take_torchs_current_stream(monkeypatch):
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 1000 + device, raising=False)
     assert mb._stream_for(OnGpu(), None) == 1003 and mb._stream_for(OnGpu(), 0) == 0 and mb._stream_for(OnGpu(), 77) == 77
     assert mb._stream_for(cpu(1), None) == 0 and mb._stream_for(A, None) == 0
+
+
+@pytest.mark.parametrize("T", [1, 70, 1000])
+def test_the_fp32_backward_asks_for_what_it_uses(T):
+    """Gates, T and P are kept with the checkpoints there: a backward needs room for a state a chunk and U's rows."""
+    d = desc(T=T, io=mb.M2RNN_F32, K=64, V=32)
+    up = lambda n: -(-n // 256) * 256
+    assert mb.m2rnn_delta_workspace_bytes(d, 1) == up(2 * 4 * -(-T // 32) * 64 * 32 * 4) + up(2 * T * 4 * 32 * 4)
