@@ -311,9 +311,10 @@ m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t group
  * k is used as it is: with beta_t |k_t|^2 <= 2 the rule does not expand, e.g. keys of unit length
  * (m2rnn_group_norm_fwd) and beta in [0, 2].  A step with g = 0 and beta = 0 leaves the state as it was: so
  * are sequences of a batch padded at their end (q, k, v of the padding finite, their y to be ignored).
- * Without checkpoints a forward of up to 12 steps (fp32: 16) runs the recurrence step by step in one launch and
- * needs no workspace (m2rnn_delta_route_string: "step"); other calls go by chunks of steps ("chunk64<half>": 64 of
- * them on fp16 operands, "chunk32<f32>": 32 in fp32).
+ * Without checkpoints a forward of few steps (6 to 16, by the number of states and their size) runs the recurrence
+ * step by step in one launch (m2rnn_delta_route_string: "step"); other calls go by chunks of steps ("chunk64<half>":
+ * 64 of them on fp16 operands, "chunk32<f32>": 32 in fp32).  Up to 12 steps (fp32: 16) need no workspace: where
+ * there is less than m2rnn_delta_workspace_bytes asks for, they run step by step.
  *
  * m2rnn_delta_bwd: gradients of  L = sum y * dy + sum HT * dHT.
  *   ckpt  what the forward wrote, or NULL: then the states are made again, in the workspace

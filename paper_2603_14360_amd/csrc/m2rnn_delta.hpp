@@ -71,7 +71,8 @@ hipError_t delta_half_fwd(const DeltaArgs &a, hipStream_t s);
 hipError_t delta_half_bwd(const DeltaArgs &a, hipStream_t s);
 
 // The recurrence step by step, the state in registers: serving, and segments of a few steps.
-bool delta_step_serves(int T, int io);
+// Up to how many steps that is the faster way.
+int delta_step_most(double states, int K, int V);
 hipError_t delta_step_fwd(const DeltaArgs &a, hipStream_t s);
 
 constexpr float kLog2e = 1.4426950408889634f;

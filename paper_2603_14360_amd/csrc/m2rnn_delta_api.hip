@@ -42,6 +42,9 @@ size_t ws_bytes(const DeltaLayout &l, int bwd) {
   const size_t fwd = (bwd && l.kept ? 0 : l.gates + l.mats) + l.carry;
   return bwd ? fwd + l.states + l.rows + l.dexps + 2 * l.heads + (bwd >= 2 ? ckpt_bytes(l) : 0) : fwd;
 }
+bool few_steps(const m2rnn_desc *d) { return d->T <= delta_step_most((double)d->B * d->N, d->K, d->V); }
+// A forward of so many steps needs no workspace: without one it runs step by step, whatever is faster.
+bool needs_no_room(const m2rnn_desc *d) { return d->T <= (d->io == M2RNN_BF16 ? 12 : 16); }
 bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }
 
 }  // namespace
@@ -58,7 +61,7 @@ size_t m2rnn_delta_workspace_bytes(const m2rnn_desc *desc, int bwd) {
 
 const char *m2rnn_delta_route_string(const m2rnn_desc *desc, int bwd) {
   if (check(desc) != M2RNN_OK) return "invalid descriptor";
-  if (!bwd && delta_step_serves(desc->T, desc->io)) return "step";
+  if (!bwd && few_steps(desc)) return "step";
   return half(args_of(desc)) ? "chunk64<half>" : "chunk32<f32>";
 }
 
@@ -74,8 +77,10 @@ m2rnn_status m2rnn_delta_fwd(const m2rnn_desc *desc, const void *q, const void *
   DeltaArgs a = args_of(desc);
   a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.H0 = H0; a.y = y; a.HT = HT;
   a.ckpt = (char *)ckpt; a.ws = (char *)workspace;
-  const bool step = !ckpt && delta_step_serves(desc->T, desc->io);
-  const size_t need = step ? 0 : ws_bytes(layout(a), 0);
+  size_t need = ws_bytes(layout(a), 0);
+  const bool room = workspace && workspace_bytes >= need;
+  const bool step = !ckpt && (few_steps(desc) || (!room && needs_no_room(desc)));
+  if (step) need = 0;
   if (need > 0 && (!workspace || workspace_bytes < need)) return workspace ? M2RNN_ERR_WORKSPACE : M2RNN_ERR_NULL;
   if (desc->B == 0) return M2RNN_OK;
   hipStream_t s = (hipStream_t)hip_stream;

@@ -123,10 +123,18 @@ hipError_t pick(const DeltaArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Up to how many steps a forward without checkpoints runs here.  us at 8, then 9 steps by chunks (which hardly depend on
-// how many they are): bf16, 32 states of 128 x 128 9.2 / 11.8, 1024 of them 36.3 / 57.3; fp32 9.0 / 14.7 and 36.0 / 114.7; a
-// step is 0.85 us, or 2.2 with 1024 states.
-bool delta_step_serves(int T, int io) { return T <= (io == 1 ? 12 : 16); }
+// Up to how many steps a forward without checkpoints runs here rather than by chunks, which hardly depend on how many
+// they are.  A step costs 0.85 us, or what the workgroups that do not fit on the chip at once make of it: about as
+// much for small heads as for large ones, whose chunks cost more.  us of 6, 8, 12 and 16 steps here | by chunks:
+//     bf16   32 states of 128 x 128   7.6   9.3  12.7  16.3 |  13.4        fp32     7.6   9.1  12.5  16.0 |  14.9
+//          1024 of 128 x 128         30.7  36.2  46.0  57.5 |  65                  31.5  37.1  47.3  58.7 | 115
+//           256 of 64 x 64            8.7  10.6  14.6  18.5 |  14.5                 8.7  10.6  14.5  18.3 |  17
+//          1024 of 32 x 32           12.5  16.1  22.3  28.8 |  20                  12.6  16.2  22.6  29.2 |  18.4
+//          5376 of 64 x 16           61.8  80.8 119   158   |  66                  61.9  80.8 119   158   |  65
+int delta_step_most(double states, int K, int V) {
+  if (K >= 32 && K * V <= 1024) return states <= 512 ? 12 : states <= 2048 ? 8 : 6;
+  return K >= 32 && V >= 64 && states * K * V >= 1 << 22 ? 16 : 12;
+}
 hipError_t delta_step_fwd(const DeltaArgs &a, hipStream_t s) {
   return a.io == 0 ? pick<float>(a, s) : pick<__hip_bfloat16>(a, s);
 }

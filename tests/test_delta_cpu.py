@@ -233,3 +233,20 @@ def test_the_fp32_backward_asks_for_what_it_uses(T):
     d = desc(T=T, io=mb.M2RNN_F32, K=64, V=32)
     up = lambda n: -(-n // 256) * 256
     assert mb.m2rnn_delta_workspace_bytes(d, 1) == up(2 * 4 * -(-T // 32) * 64 * 32 * 4) + up(2 * T * 4 * 32 * 4)
+
+
+@pytest.mark.parametrize("io", [mb.M2RNN_F32, mb.M2RNN_BF16])
+def test_few_steps_go_the_faster_way(io):
+    """Fewer steps by the recurrence where heads are small and many, whose chunks are cheap; more where the states are large."""
+    route = lambda **kw: mb.m2rnn_delta_route_string(desc(io=io, **kw), 0)
+    for B, N, K, V, most in ((1, 32, 128, 128, 12), (16, 16, 128, 128, 16), (4, 16, 64, 64, 12), (64, 16, 64, 64, 16), (1, 84, 64, 16, 12),
+                             (64, 84, 64, 16, 6), (64, 16, 32, 32, 8), (32, 16, 32, 32, 12), (256, 16, 16, 16, 12), (256, 16, 16, 64, 12)):
+        assert route(B=B, N=N, K=K, V=V, T=most) == "step" != route(B=B, N=N, K=K, V=V, T=most + 1), (B, N, K, V)
+
+
+def test_twelve_steps_need_no_workspace():
+    """... whichever way is the faster one; an empty batch of them has nothing to do, and launches nothing."""
+    none = dict(q=None, k=None, v=None, g=None, beta=None, y=None, HT=None, ws=None)
+    for io, most in ((mb.M2RNN_BF16, 12), (mb.M2RNN_F32, 16)):
+        assert fwd(desc(B=0, N=1, K=64, V=16, T=most, io=io), **none) == 0
+        assert fwd(desc(B=2, N=4, K=64, V=64, T=most + 1, io=io), ws=None) == 1

@@ -101,3 +101,21 @@ def test_calls_without_a_stream_run_on_the_current_one():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("io,T", [("bf16", 12), ("f32", 16)])
+def test_twelve_steps_without_a_workspace(io, T):
+    """Many small heads, which go by chunks from 8 steps on where there is room for it."""
+    import torch
+    B, N, K, V = 11, 50, 64, 16
+    s = dr.rule_inputs(83, B, T, N, K, V, Nqk=10, io=io)
+    d = small.device(s, io)
+    desc = mb.make_desc(B=B, T=T, N=N, K=K, V=V, Nqk=10, io=mb.M2RNN_BF16 if io == "bf16" else mb.M2RNN_F32)
+    assert mb.m2rnn_delta_route_string(desc, 0) != "step"
+    got = {"y": torch.full_like(d["v"], float("nan")), "HT": torch.full_like(d["H0"], float("nan"))}
+    mb.m2rnn_delta_fwd(desc, *(d[n] for n in ("q", "k", "v", "g", "beta", "H0")), got["y"], got["HT"], None, None,
+                       stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    y, HT, _ = dr.rule_fwd(*(s[n] for n in ("q", "k", "v", "g", "beta", "H0")))
+    small.check(got, {"y": y, "HT": HT}, (io, T))
+    small.check(small.run(s, io, backward=False), {"y": y, "HT": HT}, (io, T))
