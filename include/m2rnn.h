@@ -320,23 +320,25 @@ m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t group
  *   ckpt  what the forward wrote, or NULL: then the states are made again, in the workspace
  *   dy [B,T,N,V] io    dHT [B,N,K,V] fp32 or NULL (zero)
  *   dq, dk [B,T,Nqk,K] io (summed over the heads that share one)    dv [B,T,N,V] io
- *   dg, dbeta [B,T,N] io (bf16 too: the sums behind them are no finer there)
+ *   dg, dbeta [B,T,N] io, as the other gradients (the sums behind them carry 11 bits under bf16)
  *   dH0 [B,N,K,V] fp32, or NULL; may be dHT (segments of a sequence, from the last to the first)
  *   H0 is read only where ckpt is NULL (a forward that carried its state in place has overwritten it).
  *   workspace: m2rnn_delta_workspace_bytes(desc, 0 forward | 1 backward with ckpt | 2 without).
  *   N V and Nqk K below 2^23; B N at most 2^20 - 8, B N (T / 32 + 1) below 2^24.
- * Numbers: fp32 io is computed in fp32 throughout (and bf16 io with K = 16 or V = 16).  bf16 io feeds fp16 matrix-core
- * operands: magnitudes of q, k, v, the state and products of two keys or of a query and a key must stay below
- * 2*10^4; the states and dH0 are as good as fp32 with operands of 22 bits, other results carry the 11 bits that
- * bf16 can use.  What is smaller than 2^-14 is held to 2^-25 of one, not of itself.  Keys of unit length, queries
- * of length K^{-1/2} and v near one are far above that.  Errors (2-norm, K = 64) with q a thousand, ten thousand
- * times smaller than so: y 0.003, 0.02 instead of 0.0017, dH0 0.001, 0.01; with k: dv, dbeta 0.002, 0.014; with v and
- * H0: HT 7e-5, 7e-4.  Scale such tensors up (y is linear in q, and in v and H0), or pass fp32.
- * dy, dHT and the gradients may have any magnitude; of a sequence, gradients that are 2^-24 of the
- * largest one in the same 64 steps are lost beside it.
+ * Numbers: fp32 io is computed in fp32 throughout (and bf16 io with K = 16 or V = 16, and few steps).  Other bf16 io
+ * feeds fp16 matrix-core operands, brought near one by powers of two for each 64 steps of a head and, of what has
+ * columns of V, for 16 or 32 of those: tensors may have any magnitude, and what is 2^-25 of the largest entry of its
+ * tensor (v and the state; dy; dHT; of k 2^-21, of q 2^-18) there, or less, is lost beside it.  The states and dH0 are as good as fp32 with
+ * operands of 22 bits, other results carry the 11 bits that bf16 can use.  Errors (2-norm; q and k of unit length,
+ * or 10^4 times off that): HT, dH0 2e-7 to 4e-7, the others 0.0017, which is their rounding to bf16; where sums cancel
+ * (dg, as a difference) more, as with any operands of 11 bits.
+ * That holds while the rule does not expand: updates that grow by more than 2^10 within 64 steps, or keys there whose
+ * lengths differ by more than 10^4 with beta |k|^2 near 2, overflow.
  * A NaN or an infinity in a step reaches y of up to 63 steps before it (the steps of a chunk are computed together,
- * and what they do not see of each other is multiplied by zero), the states behind it, and the gradients of both;
- * in q and k all of the head's columns, in v and dy the column's; never another head's or batch element's.
+ * and what they do not see of each other is multiplied by zero), the states behind it, and the gradients of both: in
+ * q and k all of the head's columns, in v, H0, dy and dHT y, HT, dv and dH0 of its column alone, but dq, dk, dg and
+ * dbeta, which are sums over the columns, as a whole.  Never another head's (dq and dk: one that shares q and k)
+ * or batch element's.
  * The same call gives the same bits (no atomics).
  * Errors as for the scan; M2RNN_ERR_CHUNK for a chunk that is not 0.
  */

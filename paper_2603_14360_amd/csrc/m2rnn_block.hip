@@ -67,7 +67,8 @@ inline ConvPlan conv_plan(int B, int T, int C, int most_rows) {
 
 // WIN: the steps in front of the first are the rows of `win` [B,3,C] and not zeros, and the last three go
 // to `win_out`, both by the item that starts a batch row: it has read all of `win` when it writes, and no other
-// item reads it, so the two may be one buffer.  64 single steps of 1472 channels: 4.5 us, the launch; 4 x 777: 8.1.
+// item reads it, so the two may be one buffer.  64 single steps of 1472 channels: 4.0 us, the launch; 4 x 777: 7.7
+// (a kernel by itself; calls in a row overlap in their ramps).
 template <typename IO, bool WIN>
 __global__ void __launch_bounds__(kThreads)
     conv_silu_fwd_kernel(const void *__restrict__ x, const void *__restrict__ w,

@@ -76,10 +76,10 @@ __device__ __forceinline__ h8_t bf16_to_h8(u4_t w) {
   return __builtin_bit_cast(h8_t, r);
 }
 // Keys and queries of a chunk whose largest entry has an exponent e far from zero come as fp16 over 2^e, others as they
-// are: entries of 2^-17 and more are exact then, and of keys 2^-21 of the largest one is lost at most, of queries,
-// which reach nothing but bf16 results and dH0, 2^-15.
+// are: entries of 2^-17 and more are exact then, and below them 2^-25 is lost, 2^-21 of the largest key's entry at most,
+// 2^-18 of the largest query's (K^{-1/2} of a unit vector's, for which there is more room).
 __device__ __forceinline__ bool far_key(int e) { return e < -4 || e > 10; }
-__device__ __forceinline__ bool far_query(int e) { return e < -10 || e > 10; }
+__device__ __forceinline__ bool far_query(int e) { return e < -7 || e > 10; }
 template <bool FAR, int N>
 __device__ __forceinline__ void rows_to_h8(const u4_t (&w)[N], int e, h8_t (&x)[N]) {
   const float s = two_to(-e);
@@ -198,7 +198,7 @@ __device__ __forceinline__ f4_t mma_f32(f4_t a, f4_t b, f4_t c) {
 //     [ T0 0 ; -T1 A10 T0  T1 ]   for the two pairs of neighbours, and the same with blocks of 32,
 // whose products run on the fp32 matrix instructions; T takes the place of A in LDS block by block.
 // What bounds it is latency: all loads are issued at once, and 24 KB of LDS leave room for six workgroups per CU.
-// 8 x 4096 steps, 16 heads of 64 x 64: 65 us forward, 98 backward (3.5 TB/s, mostly of T and P).
+// 8 x 4096 steps, 16 heads of 64 x 64: 69 us forward, 94 backward (3.5 TB/s, mostly of T and P).
 struct PrepLds {
   float As[C][C + 4], Xt[C / 2][C / 2 + 4], hi[C], lo[C], be[C], tops[12];
 };
@@ -572,8 +572,8 @@ struct Part {
   const float *H0;
   float *HT;
 };
-// Y: y is wanted;  CKPT: the chunks' states and U are.  8 x 4096 steps, 16 heads of 64 x 64: 163 us, 2.5 a chunk on
-// 256 workgroups (3.5 TB/s); 65 536 steps, 32 of 64 x 64 without checkpoints: 1.4 a chunk on 128 of them,
+// Y: y is wanted;  CKPT: the chunks' states and U are.  8 x 4096 steps, 16 heads of 64 x 64: 167 us, 2.6 a chunk on
+// 256 workgroups (3.4 TB/s); 65 536 steps, 32 of 64 x 64 without checkpoints: 1.4 a chunk on 128 of them,
 // T and P of later chunks beside it.
 template <int K, int VB, bool Y, bool CKPT>
 __global__ void __launch_bounds__(256, 2)
@@ -909,7 +909,7 @@ __global__ void __launch_bounds__(256, 2)
 }
 
 // Backward, chunks in reverse order.  As in the forward dH lies in registers over 2^ed and enters as that, dy over 2^ey, dU
-// and Z over 2^ez.  8 x 4096 steps, 16 heads of 64 x 64: 235 us, 3.7 a chunk (3.5 TB/s).
+// and Z over 2^ez.  8 x 4096 steps, 16 heads of 64 x 64: 216 us, 3.4 a chunk (3.8 TB/s).
 template <int K, int VB>
 constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 7 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 12 * 4; }
 
@@ -1282,9 +1282,9 @@ __global__ void __launch_bounds__(256, 2)
 // ------------------------------------------------------------------ dq, dk, dg, dbeta of one chunk
 // Wave w has the chunk's steps 16 w .. 16 w + 15 and all of K: D[row of K][step].  S1 and S2 go through LDS to
 // the operands that the last products take.  With V <= 64 the products with H and dH come after that, in a loop of
-// their own: with all loads of a short loop in flight the two are faster (8 x 4096 steps, 16 heads of 64 x 64: 185 us,
+// their own: with all loads of a short loop in flight the two are faster (8 x 4096 steps, 16 heads of 64 x 64: 186 us,
 // 4.4 TB/s, against 198 in one).  With more blocks of 32 columns the second reading of y, z and U costs more than that
-// gives (4 x 8192, 8 of 128 x 128: 294 us against 223 in one loop).
+// gives (4 x 8192, 8 of 128 x 128: 294 us against 225 in one loop).
 template <int K>
 constexpr int lds_grad() { return (2 * C * (K + 8) + 2 * C * LC + C) * 2 + (6 * C + 4 * 4) * 4; }
 
@@ -1583,16 +1583,19 @@ Ws carve(const DeltaLayout &l, char *p) {
 }
 
 // Columns of V per workgroup of the kernels that run in order: 32, or 16 where that leaves half of the 256 CUs
-// without one.  us, forward / backward kernel, 32 -> 16 columns: 32 states of 128 x 128, 8192 steps 333 / 467 ->
-// 277 / 403 (128 workgroups of 32 columns); 128 of 64 x 64, 4096 steps 163 / 231 -> 230 / 260 (256).
+// without one.  us, forward + backward of 1024 steps, 32 -> 16 columns, by the workgroups that there are with 32:
+//                32           64          128          160          256          512
+//   32 x 32    96 ->  84   104 ->  92   122 -> 112   130 -> 132   165 -> 167   329 -> 371
+//   64 x 64   103 ->  84   114 ->  94   132 -> 114   138 -> 139   163 -> 165   300 -> 333
+//  128 x 128  130 -> 108   135 -> 112   149 -> 126   165 -> 182   184 -> 199   355 -> 405
 int columns(const DeltaArgs &a) {
   return a.B * a.N * (a.V / 32) <= 128 ? 16 : 32;
 }
 // Chunks per launch of the forward.  Where its chains have no more than half of the CUs, a long one goes in parts whose
 // launches also form T and P of the next part, on the idle CUs: in parts of about 1024 chunks over all states, as many
 // as run at once (longer ones keep the chains' CUs busy as well), and of 16 each at least, for a launch's 6 us.
-// us, whole -> parts of half, once, twice as many: 65 536 steps of 32 states 64 x 64 1648 -> 1537, 1413, 1548; 32 768 of
-// 16 of 64 x 128 646 -> 612, 586, 621; of 8 of 128 x 128 852 -> 835, 816, -.  With chains on all 256 CUs there is
+// us, whole -> parts of half, once, twice as many: 65 536 steps of 32 states 64 x 64 1592 -> 1631, 1471, 1462; 32 768 of
+// 16 of 64 x 128 675 -> 718, 679, 670; of 8 of 128 x 128 823 -> 837, 821, 819.  With chains on all 256 CUs there is
 // nothing to gain (8 x 4096 steps, 16 of 64 x 64: 231 -> 228 to 241).
 int part_chunks(const DeltaArgs &a, int chunks) {
   const int units = a.B * a.N;

@@ -21,7 +21,8 @@ namespace m2rnn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 1024;  // most partial rows of dw, db; with one slice per token four workgroups per CU
+// most partial rows of dw, db; with one slice per token four workgroups per CU, which in bf16 all run at once (fp32: three)
+constexpr int kRows = 1024;
 
 struct NormPlan {
   int L, LV;     // channels and vectors of a group
