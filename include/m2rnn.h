@@ -327,11 +327,12 @@ m2rnn_status m2rnn_group_norm_bwd(int32_t B, int32_t T, int32_t D, int32_t group
  *   N V and Nqk K below 2^23; B N at most 2^20 - 8, B N (T / 32 + 1) below 2^24.
  * Numbers: fp32 io is computed in fp32 throughout (and bf16 io with K = 16 or V = 16, and few steps).  Other bf16 io
  * feeds fp16 matrix-core operands, brought near one by powers of two for each 64 steps of a head and, of what has
- * columns of V, for 16 or 32 of those: tensors may have any magnitude, and what is 2^-25 of the largest entry of its
- * tensor (v and the state; dy; dHT; of k 2^-21, of q 2^-18) there, or less, is lost beside it.  The states and dH0 are as good as fp32 with
- * operands of 22 bits, other results carry the 11 bits that bf16 can use.  Errors (2-norm; q and k of unit length,
- * or 10^4 times off that): HT, dH0 2e-7 to 4e-7, the others 0.0017, which is their rounding to bf16; where sums cancel
- * (dg, as a difference) more, as with any operands of 11 bits.
+ * columns of V, for 16 or 32 of those.  Tensors may have any magnitude; within such 64 steps what is 2^-25 of the
+ * largest entry, or less, is lost beside it: of v and the state together; of dy and the gradient of the state together
+ * (but for dq, which has dy alone); of k 2^-21, of q 2^-18.  The states and dH0 are as good as fp32 with operands of 22
+ * bits, other results carry the 11 bits that bf16 can use.  Errors (2-norm; k of unit length or a hundredth of it, q of
+ * length K^{-1/2} and v near one, or 10^4 times larger or smaller): HT, dH0 1e-7 to 4e-7, the others 0.0017, which is
+ * their rounding to bf16; dg, where the sums that it is the difference of are larger, more.
  * That holds while the rule does not expand: updates that grow by more than 2^10 within 64 steps, or keys there whose
  * lengths differ by more than 10^4 with beta |k|^2 near 2, overflow.
  * A NaN or an infinity in a step reaches y of up to 63 steps before it (the steps of a chunk are computed together,

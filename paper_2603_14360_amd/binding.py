@@ -353,6 +353,7 @@ def m2rnn_delta_route_string(desc, bwd):
 
 
 def m2rnn_delta_fwd(desc, q, k, v, g, beta, H0, y, HT, ckpt, workspace, stream=None, check=True):
+    """Raw call, as m2rnn_fwd: tensors are taken as they are, stream None is the null stream."""
     rc = lib().m2rnn_delta_fwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(H0),
                                _ptr(y), _ptr(HT), _ptr(ckpt), _ptr(workspace), _nbytes(workspace), stream or 0)
     return _check(rc, "m2rnn_delta_fwd", check)
@@ -360,6 +361,7 @@ def m2rnn_delta_fwd(desc, q, k, v, g, beta, H0, y, HT, ckpt, workspace, stream=N
 
 def m2rnn_delta_bwd(desc, q, k, v, g, beta, H0, ckpt, dy, dHT, dq, dk, dv, dg, dbeta, dH0, workspace, stream=None,
                     check=True):
+    """Raw call, as m2rnn_delta_fwd."""
     rc = lib().m2rnn_delta_bwd(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(H0),
                                _ptr(ckpt), _ptr(dy), _ptr(dHT), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dg),
                                _ptr(dbeta), _ptr(dH0), _ptr(workspace), _nbytes(workspace), stream or 0)
