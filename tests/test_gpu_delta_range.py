@@ -159,3 +159,69 @@ def test_what_is_not_finite_stays_in_its_column(io, where, bad):
         assert not np.isfinite(g["dk"][1, :t - 63, 2]).all(-1).any()
     else:
         assert not np.isfinite(g["HT"][1, 2, :, col]).all() and not np.isfinite(g["y"][1, t:, 2, col]).any()
+
+
+# (B, N, K, V): 16 and 32 columns of V per workgroup, all sizes of K
+LONG = [(2, 3, 64, 64), (2, 2, 128, 32), (3, 2, 32, 256), (33, 4, 64, 32), (17, 2, 128, 128), (33, 4, 32, 32)]
+
+
+def check_chunks(got, want, names, label):
+    """Every 64 steps by the largest entry there."""
+    for t in range(0, want["y"].shape[1], 64):
+        small.check({n: got[n][:, t:t + 64] for n in names}, {n: want[n][:, t:t + 64] for n in names}, (label, t))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N,K,V", LONG)
+@pytest.mark.parametrize("first,last", [(128, 192), (0, 64), (256, 300)])
+def test_keys_and_queries_far_from_one_in_some_steps(io, B, N, K, V, first, last):
+    """... between chunks where they are near it."""
+    print("case", io, B, N, K, V, first, flush=True)
+    s = dr.rule_inputs(69, B, 300, N, K, V, io=io)
+    s["q"][:, first:last] *= np.float32(2.0 ** -14)
+    s["k"][:, first:last] *= np.float32(2.0 ** -9)
+    s["beta"][:, first:last] *= np.float32(2.0 ** 18)
+    s["v"][:, first:last] *= np.float32(2.0 ** -9)
+    want, got = dr.rule(s), small.run(s, io)
+    small.check({n: got[n] for n in ("HT", "dH0")}, {n: want[n] for n in ("HT", "dH0")}, (io, "states"))
+    check_chunks(got, want, ("y", "dq", "dv"), (io, K, V, first))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N,K,V", LONG)
+def test_states_and_gradients_that_change_their_size(io, B, N, K, V):
+    """v and dy 2^20 times larger for some steps, a reset behind them: both recurrences go up and down again."""
+    print("case", io, B, N, K, V, flush=True)
+    s = dr.rule_inputs(70, B, 400, N, K, V, io=io)
+    for n in ("v", "dy"):
+        s[n][:, 150:170] *= np.float32(2.0 ** 20)
+    s["g"][:, 140] = s["g"][:, 200] = -np.inf
+    want, got = dr.rule(s), small.run(s, io)
+    small.check({"HT": got["HT"]}, {"HT": want["HT"]}, (io, "states"))
+    check_chunks(got, want, ("y", "dq"), (io, K, V))
+    # bf16 io: the steps 128 to 139, which alone reach what is in front of them, share their 64 steps with losses 2^20
+    # times larger and are held to 2^-25 of those, in dy and once more in Z.  What dH is off by in front of them, at
+    # most the sum of |q_t| times that, twice, decays by e^g (the rule does not expand), and keys of unit length hand
+    # it on to dv, times beta below one.
+    lost = 2 * 2.0 ** -25 * np.abs(s["dy"]).max() * np.abs(s["q"][:, 128:140]).max(-1).sum(1).max() if io == "bf16" else 0.0
+    decay = np.exp(s["g"][:, :128][:, ::-1].cumsum(1)[:, ::-1])  # from step t to 128
+    off = small.F32 * np.abs(want["dH0"]).max() + lost * decay[:, 0].max()
+    assert np.abs(gu.to_np(got["dH0"]) - want["dH0"]).max() <= off
+    for t in range(0, 400, 64):
+        g, w = gu.to_np(got["dv"][:, t:t + 64]), want["dv"][:, t:t + 64]
+        more = np.abs(s["k"][:, t:t + 64]).sum(-1).max() * lost * decay[:, t:t + 64].max() if t < 128 else 0.0
+        rel = small.BF16 * (np.abs(w) + np.abs(w).max()) if io == "bf16" else small.F32 * np.abs(w).max()
+        assert (np.abs(g - w) <= rel + more).all(), t
+
+
+@pytest.mark.parametrize("B,N,K,V", LONG)
+def test_an_infinity_far_behind(B, N, K, V):
+    """... in v and in dy of one column each: other columns of all chunks are right, also where the state was scaled anew."""
+    s = dr.rule_inputs(73, B, 300, N, K, V, io="bf16")
+    want = dr.rule(s)
+    s["v"][0, 70, 0, 3], s["dy"][0, 230, 0, 9] = np.inf, -np.inf
+    got = small.run(s, "bf16")
+    keep = [c for c in range(V) if c not in (3, 9)]
+    pick = lambda x, n: x[..., keep] if n in ("y", "dv", "HT", "dH0") else x[:, :, 1:]
+    names = ("y", "dv", "HT", "dH0", "dq", "dk", "dbeta")
+    small.check({n: pick(got[n], n) for n in names}, {n: pick(want[n], n) for n in names}, (K, V))
