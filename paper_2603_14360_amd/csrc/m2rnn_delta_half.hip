@@ -198,7 +198,7 @@ __device__ __forceinline__ f4_t mma_f32(f4_t a, f4_t b, f4_t c) {
 //     [ T0 0 ; -T1 A10 T0  T1 ]   for the two pairs of neighbours, and the same with blocks of 32,
 // whose products run on the fp32 matrix instructions; T takes the place of A in LDS block by block.
 // What bounds it is latency: all loads are issued at once, and 24 KB of LDS leave room for six workgroups per CU.
-// 8 x 4096 steps, 16 heads of 64 x 64: 69 us forward, 94 backward (3.5 TB/s, mostly of T and P).
+// 8 x 4096 steps, 16 heads of 64 x 64: 69 us forward, 93 backward (3.5 TB/s, mostly of T and P).
 struct PrepLds {
   float As[C][C + 4], Xt[C / 2][C / 2 + 4], hi[C], lo[C], be[C], tops[12];
 };
@@ -574,9 +574,10 @@ struct Part {
 };
 // Y: y is wanted;  CKPT: the chunks' states and U are.  8 x 4096 steps, 16 heads of 64 x 64: 167 us, 2.6 a chunk on
 // 256 workgroups (3.4 TB/s); 65 536 steps, 32 of 64 x 64 without checkpoints: 1.4 a chunk on 128 of them,
-// T and P of later chunks beside it.
+// T and P of later chunks beside it.  K = 64, VB = 32: three workgroups fit into a CU's LDS, and are given registers for it
+// (64 sequences of 64 steps, 16 heads, a call without checkpoints 37.2 -> 35.1).
 template <int K, int VB, bool Y, bool CKPT>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, VB == 32 && K == 64 ? 3 : 2)
     delta_half_fwd_kernel(DeltaArgs a, int chunks, Part p, float *gates, half_t *mats, half_t *__restrict__ states,
                           half_t *__restrict__ rows_u, int *__restrict__ exps) {
   using S = Scan<K, VB>;
@@ -610,10 +611,15 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
   for (int i = 0; i < KTW; ++i)
 #pragma unroll
-    for (int j = 0; j < VTW; ++j)
+    for (int j = 0; j < VTW; ++j) H[i][j] = zero;
+  if (p.H0)
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        H[i][j][x] = p.H0 ? p.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          H[i][j][x] = p.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)];
   // (here, and not at the head of the loop, which would then wait for everything in each of its rounds)
 #pragma unroll
   for (int i = 0; i < KTW; ++i)
@@ -710,10 +716,14 @@ __global__ void __launch_bounds__(256, 2)
     eh = to;
   };
   if (p.c0 < p.c1) {
-    int et, ev;
-    measure(et, ev);
-    er = scale_of_u(et, ev);
-    rescale(scale_of_state(et, er));
+    top_of_wave(red + 4, H, vf, wv);
+    lds_barrier();
+    const uint32_t tops = top_of_all(red + 4);
+    if (!not_finite(tops)) {  // (else the first round measures again)
+      const int et = top_exponent(tops >> 16);
+      er = scale_of_u(et, top_exponent(tops));
+      rescale(scale_of_state(et, er));
+    }
   }
   const int w = place(wv);
   auto is_far = [&]() { return far_key(ek) || (Y && far_query(eq)); };
@@ -909,9 +919,13 @@ __global__ void __launch_bounds__(256, 2)
 }
 
 // Backward, chunks in reverse order.  As in the forward dH lies in registers over 2^ed and enters as that, dy over 2^ey, dU
-// and Z over 2^ez.  8 x 4096 steps, 16 heads of 64 x 64: 216 us, 3.4 a chunk (3.8 TB/s).
+// and Z over 2^ez.  8 x 4096 steps, 16 heads of 64 x 64: 217 us, 3.4 a chunk (3.8 TB/s).
+// (own_z: Z has room of its own, and the waves need not wait for each other before the next chunk's inputs come; with K = 128
+// and VB = 32 it takes W's place, so that two workgroups fit into a CU's LDS: 4 x 64 steps of 32 heads 16.2 -> 12.4 us)
 template <int K, int VB>
-constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + 7 * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 12 * 4; }
+constexpr bool own_z() { return K != 128 || VB != 32; }
+template <int K, int VB>
+constexpr int lds_bwd() { return (2 * C * (K + 8) + 2 * VB * (K + 8) + (own_z<K, VB>() ? 7 : 5) * VB * LC + 4 * Turn<VB>::HALFS) * 2 + 4 * 64 * 4 + 12 * 4; }
 
 template <int K, int VB>
 __global__ void __launch_bounds__(256, 2)
@@ -922,7 +936,7 @@ __global__ void __launch_bounds__(256, 2)
   extern __shared__ __align__(16) char lds[];
   half_t *ks = (half_t *)lds, *qs = ks + C * LK, *Ht = qs + C * LK, *Hl = Ht + VB * LK, *Yt = Hl + VB * LK;
   half_t *Wt = Yt + VB * LC, *Wl = Wt + VB * LC, *Ut = Wl + VB * LC, *Ul = Ut + VB * LC;
-  half_t *Zt = Ul + VB * LC, *Zl = Zt + VB * LC, *turn = Zl + VB * LC;
+  half_t *Zt = own_z<K, VB>() ? Ul + VB * LC : Wt, *Zl = Zt + VB * LC, *turn = (own_z<K, VB>() ? Zl : Ul) + VB * LC;
   uint32_t *red = (uint32_t *)(turn + 4 * Turn<VB>::HALFS) + 4 * 64;
   int unit, part;
   if (!delta_map(a.B * a.N, a.V / VB, unit, part)) return;
@@ -941,10 +955,15 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
   for (int i = 0; i < KTW; ++i)
 #pragma unroll
-    for (int j = 0; j < VTW; ++j)
+    for (int j = 0; j < VTW; ++j) D[i][j] = zero;
+  if (a.dHT)
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        D[i][j][x] = a.dHT ? a.dHT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)] : 0.f;
+    for (int i = 0; i < KTW; ++i)
+#pragma unroll
+      for (int j = 0; j < VTW; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          D[i][j][x] = a.dHT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)];
   // (here, and not at the head of the loop, which would then wait for everything in each of its rounds)
 #pragma unroll
   for (int i = 0; i < KTW; ++i)
@@ -1045,10 +1064,15 @@ __global__ void __launch_bounds__(256, 2)
     fetch2(chunks - 1);
     fetch3(chunks - 1);
     take1(std::false_type());
-    int td;
-    measure(td, ey);
-    ez = scale_of_z(td, ey);
-    rescale(scale_of_dh(td, ey, ez));
+    top_of_wave(red + 4, D, yf, wv);
+    lds_barrier();
+    const uint32_t tops = top_of_all(red + 4);
+    if (!not_finite(tops)) {  // (else the first round measures again)
+      const int td = top_exponent(tops >> 16);
+      ey = top_exponent(tops);
+      ez = scale_of_z(td, ey);
+      rescale(scale_of_dh(td, ey, ez));
+    }
   }
   auto is_far = [&]() { return far_key(ek) || far_query(eq); };
   // the chunks from ch down, as in the forward
@@ -1257,6 +1281,7 @@ __global__ void __launch_bounds__(256, 2)
     // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
     __builtin_amdgcn_raw_buffer_store_b128(u4_t{(uint32_t)ed, (uint32_t)ez, (uint32_t)ey, 0u}, __builtin_amdgcn_make_buffer_rsrc(
                                            exps + at * (a.V / VB) + part, 0, 16, 0x00027000), 16 * (int)threadIdx.x, 0, 0);
+    if (!own_z<K, VB>()) lds_barrier();
     --ch;
     if (!FAR && is_far()) break;
    }
@@ -1282,7 +1307,7 @@ __global__ void __launch_bounds__(256, 2)
 // ------------------------------------------------------------------ dq, dk, dg, dbeta of one chunk
 // Wave w has the chunk's steps 16 w .. 16 w + 15 and all of K: D[row of K][step].  S1 and S2 go through LDS to
 // the operands that the last products take.  With V <= 64 the products with H and dH come after that, in a loop of
-// their own: with all loads of a short loop in flight the two are faster (8 x 4096 steps, 16 heads of 64 x 64: 186 us,
+// their own: with all loads of a short loop in flight the two are faster (8 x 4096 steps, 16 heads of 64 x 64: 188 us,
 // 4.4 TB/s, against 198 in one).  With more blocks of 32 columns the second reading of y, z and U costs more than that
 // gives (4 x 8192, 8 of 128 x 128: 294 us against 225 in one loop).
 template <int K>
@@ -1336,8 +1361,12 @@ __global__ void __launch_bounds__(256, K <= 64 ? 3 : 2)
   const int eD = __builtin_amdgcn_readlane(et, 32), eZ = __builtin_amdgcn_readlane(et, 48);
   const int fl = __builtin_bit_cast(unsigned short, (half_t)two_to(el - et));
   auto own_factor = [&](int kind, int vb) {
-    const half_t f = __builtin_bit_cast(half_t, (unsigned short)__shfl(fl, 16 * kind + (vbs == 32 ? vb : 2 * vb + (g4 >> 1)), 64));
-    return h8_t{f, f, f, f, f, f, f, f};
+    const int at = 16 * kind + (vbs == 32 ? vb : 2 * vb);
+    int f;
+    if (ONE) f = __shfl(fl, at + (vbs == 32 ? 0 : g4 >> 1), 64);
+    else f = vbs == 32 || g4 < 2 ? __builtin_amdgcn_readlane(fl, at) : __builtin_amdgcn_readlane(fl, at + 1);  // (at: a constant)
+    const half_t h = __builtin_bit_cast(half_t, (unsigned short)f);
+    return h8_t{h, h, h, h, h, h, h, h};
   };
   const int *gt_tops = (const int *)gates + at * kGates + kTops;
   const int eb = gt_tops[1], ek = far_key(gt_tops[0]) ? gt_tops[0] : 0, eq = far_query(gt_tops[3]) ? gt_tops[3] : 0;
