@@ -262,9 +262,11 @@ __device__ __forceinline__ void prep_chunk(const DeltaArgs &a, int chunks, int u
   }
   __syncthreads();
   if (threadIdx.x == 0) {
+    // (keys or queries that are all zero, as behind the end of a padded sequence, need no power of two: as near one)
+    auto exponent = [](f4_t tops) { return tops[0] + tops[1] + tops[2] + tops[3] == 0.f ? 0 : exponent_of(tops); };
     int *tops = (int *)(gates + slot * kGates) + kTops;
-    tops[0] = exponent_of(*(const f4_t *)lds.tops);
-    tops[3] = exponent_of(*(const f4_t *)(lds.tops + 4));
+    tops[0] = exponent(*(const f4_t *)lds.tops);
+    tops[3] = exponent(*(const f4_t *)(lds.tops + 4));
   }
   f4_t ps[4];  // P's four columns (rows, transposed) per tile
   const int mine = 16 * wv + d;
@@ -620,7 +622,7 @@ __global__ void __launch_bounds__(256, VB == 32 && K == 64 ? 3 : 2)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           H[i][j][x] = p.H0[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)];
-  // (here, and not at the head of the loop, which would then wait for everything in each of its rounds)
+  // (here, and not at the head of the loop, which would then wait for everything at every chunk)
 #pragma unroll
   for (int i = 0; i < KTW; ++i)
 #pragma unroll
@@ -719,7 +721,7 @@ __global__ void __launch_bounds__(256, VB == 32 && K == 64 ? 3 : 2)
     top_of_wave(red + 4, H, vf, wv);
     lds_barrier();
     const uint32_t tops = top_of_all(red + 4);
-    if (!not_finite(tops)) {  // (else the first round measures again)
+    if (!not_finite(tops)) {  // (else the first chunk measures again)
       const int et = top_exponent(tops >> 16);
       er = scale_of_u(et, top_exponent(tops));
       rescale(scale_of_state(et, er));
@@ -728,7 +730,7 @@ __global__ void __launch_bounds__(256, VB == 32 && K == 64 ? 3 : 2)
   const int w = place(wv);
   auto is_far = [&]() { return far_key(ek) || (Y && far_query(eq)); };
   // the chunks from ch on; without FAR up to one whose keys or queries are far from one.  Returns the next chunk.
-  auto rounds = [&](auto far, int ch) __attribute__((always_inline)) {
+  auto run_chunks = [&](auto far, int ch) __attribute__((always_inline)) {
    constexpr bool FAR = decltype(far)::value;
    while (ch < p.c1) {
     const int next = min(ch + 1, p.c1 - 1), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
@@ -902,10 +904,10 @@ __global__ void __launch_bounds__(256, VB == 32 && K == 64 ? 3 : 2)
    return ch;
   };
   int ch = p.c0;
-  if (ch < p.c1 && !is_far()) ch = rounds(std::false_type(), ch);
+  if (ch < p.c1 && !is_far()) ch = run_chunks(std::false_type(), ch);
   if (ch < p.c1) {
     take_keys(std::true_type());
-    rounds(std::true_type(), ch);
+    run_chunks(std::true_type(), ch);
   }
   rescale(0);
   if (p.HT && S::on(wv))
@@ -964,7 +966,7 @@ __global__ void __launch_bounds__(256, 2)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           D[i][j][x] = a.dHT[state0 + (size_t)(16 * S::kt(wv, i) + 4 * g4 + x) * a.V + 16 * S::vt(wv, j)];
-  // (here, and not at the head of the loop, which would then wait for everything in each of its rounds)
+  // (here, and not at the head of the loop, which would then wait for everything at every chunk)
 #pragma unroll
   for (int i = 0; i < KTW; ++i)
 #pragma unroll
@@ -1067,7 +1069,7 @@ __global__ void __launch_bounds__(256, 2)
     top_of_wave(red + 4, D, yf, wv);
     lds_barrier();
     const uint32_t tops = top_of_all(red + 4);
-    if (!not_finite(tops)) {  // (else the first round measures again)
+    if (!not_finite(tops)) {  // (else the first chunk measures again)
       const int td = top_exponent(tops >> 16);
       ey = top_exponent(tops);
       ez = scale_of_z(td, ey);
@@ -1076,7 +1078,7 @@ __global__ void __launch_bounds__(256, 2)
   }
   auto is_far = [&]() { return far_key(ek) || far_query(eq); };
   // the chunks from ch down, as in the forward
-  auto rounds = [&](auto far, int ch) __attribute__((always_inline)) {
+  auto run_chunks = [&](auto far, int ch) __attribute__((always_inline)) {
    constexpr bool FAR = decltype(far)::value;
    while (ch >= 0) {
     const int next = max(ch - 1, 0), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
@@ -1288,10 +1290,10 @@ __global__ void __launch_bounds__(256, 2)
    return ch;
   };
   int ch = chunks - 1;
-  if (ch >= 0 && !is_far()) ch = rounds(std::false_type(), ch);
+  if (ch >= 0 && !is_far()) ch = run_chunks(std::false_type(), ch);
   if (ch >= 0) {
     take_rows(std::true_type());
-    rounds(std::true_type(), ch);
+    run_chunks(std::true_type(), ch);
   }
   rescale(0);
   if (a.dH0 && S::on(wv))

@@ -225,3 +225,21 @@ def test_an_infinity_far_behind(B, N, K, V):
     pick = lambda x, n: x[..., keep] if n in ("y", "dv", "HT", "dH0") else x[:, :, 1:]
     names = ("y", "dv", "HT", "dH0", "dq", "dk", "dbeta")
     small.check({n: pick(got[n], n) for n in names}, {n: pick(want[n], n) for n in names}, (K, V))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N,K,V", LONG)
+def test_padding_of_zeros(io, B, N, K, V):
+    """Two chunks of zeros behind a sequence and one in front: the same bits as without those behind."""
+    import torch
+    s = dr.rule_inputs(74, B, 300, N, K, V, io=io)
+    for n in ("q", "k", "v", "dy", "g", "beta"):
+        s[n][:, :64] = 0
+        s[n][:, 172:] = 0
+    short = {n: x if n in ("H0", "dHT") else x[:, :172] for n, x in s.items()}
+    got, want = small.run(s, io), small.run(short, io)
+    for n in ("HT", "dH0"):
+        assert torch.equal(got[n], want[n]), n
+    for n in ("y", "dq", "dv", "dk", "dg", "dbeta"):
+        assert torch.equal(got[n][:, :172], want[n]), n
+    small.check(want, dr.rule(short), (io, B, N, K, V))
