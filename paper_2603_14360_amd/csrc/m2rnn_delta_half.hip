@@ -731,177 +731,177 @@ __global__ void __launch_bounds__(256, VB == 32 && K == 64 ? 3 : 2)
   auto is_far = [&]() { return far_key(ek) || (Y && far_query(eq)); };
   // the chunks from ch on; without FAR up to one whose keys or queries are far from one.  Returns the next chunk.
   auto run_chunks = [&](auto far, int ch) __attribute__((always_inline)) {
-   constexpr bool FAR = decltype(far)::value;
-   while (ch < p.c1) {
-    const int next = min(ch + 1, p.c1 - 1), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
-    put_state();
-#pragma unroll
-    for (int i = 0; i < KB; ++i) *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
-    top_of_wave(red, H, vf, wv);
-    lds_barrier();  // the state is there, and k of the chunk before has been read
-    // R = beta (v - e^G K H): D[step][column]
-    const uint32_t tops = top_of_all(red);
-    h8_t hh[VT][KB], hl[VT][KB];
-    f4_t x[VT], xl[VT];
-    auto keys_with_state = [&]() {
-#pragma unroll
-      for (int t = 0; t < VT; ++t) x[t] = xl[t] = zero;
-#pragma unroll
-      for (int i = 0; i < KB; ++i)
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          x[t] = mfma_k32(kf[i], hh[t][i], x[t]);
-          xl[t] = mfma_k32(kf[i], hl[t][i], xl[t]);
-        }
-    };
-    get_state(hh, hl);
-    fetch1(next);
-    keys_with_state();
-    f4_t gh = two_to(eh + kx) * ge, br = two_to(-er) * be;
-    int et = eh + top_exponent(tops >> 16), ev = top_exponent(tops), tu = scale_of_u(et, ev);
-    int want = scale_of_state(et, tu);
-    if (not_finite(tops) | (want < eh - 2) | (want > eh + 13) | (tu < er - 3) | (tu > er + 4)) {  // (the same in all waves)
-      measure(et, ev);
-      er = scale_of_u(et, ev);
-      rescale(scale_of_state(et, er));
+    constexpr bool FAR = decltype(far)::value;
+    while (ch < p.c1) {
+      const int next = min(ch + 1, p.c1 - 1), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
       put_state();
-      lds_barrier();
+#pragma unroll
+      for (int i = 0; i < KB; ++i) *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
+      top_of_wave(red, H, vf, wv);
+      lds_barrier();  // the state is there, and k of the chunk before has been read
+      // R = beta (v - e^G K H): D[step][column]
+      const uint32_t tops = top_of_all(red);
+      h8_t hh[VT][KB], hl[VT][KB];
+      f4_t x[VT], xl[VT];
+      auto keys_with_state = [&]() {
+#pragma unroll
+        for (int t = 0; t < VT; ++t) x[t] = xl[t] = zero;
+#pragma unroll
+        for (int i = 0; i < KB; ++i)
+#pragma unroll
+          for (int t = 0; t < VT; ++t) {
+            x[t] = mfma_k32(kf[i], hh[t][i], x[t]);
+            xl[t] = mfma_k32(kf[i], hl[t][i], xl[t]);
+          }
+      };
       get_state(hh, hl);
+      fetch1(next);
       keys_with_state();
-      gh = two_to(eh + kx) * ge;
-      br = two_to(-er) * be;
-    }
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      const Pair4 s = split4(br * (vf[t] - gh * (x[t] + xl[t])));
-      *(u2_t *)&Rt[(16 * t + d) * LC + w] = s.hi;
-      *(u2_t *)&Rl[(16 * t + d) * LC + w] = s.lo;
-    }
-    lds_barrier();
-    // U = T R: D[step][column];  off the chain (Q H)^T: D[column][step]
-    h8_t rh[VT][2], rl[VT][2], hs[KTW], kT[KTW][2];
-    f4_t y[VT], u[VT], ul[VT];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      f4_t gh = two_to(eh + kx) * ge, br = two_to(-er) * be;
+      int et = eh + top_exponent(tops >> 16), ev = top_exponent(tops), tu = scale_of_u(et, ev);
+      int want = scale_of_state(et, tu);
+      if (not_finite(tops) | (want < eh - 2) | (want > eh + 13) | (tu < er - 3) | (tu > er + 4)) {  // (the same in all waves)
+        measure(et, ev);
+        er = scale_of_u(et, ev);
+        rescale(scale_of_state(et, er));
+        put_state();
+        lds_barrier();
+        get_state(hh, hl);
+        keys_with_state();
+        gh = two_to(eh + kx) * ge;
+        br = two_to(-er) * be;
+      }
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
-        const int o = (16 * t + d) * LC + 32 * kb + 8 * g4;
-        rh[t][kb] = ld8(Rt + o);
-        rl[t][kb] = ld8(Rl + o);
+        const Pair4 s = split4(br * (vf[t] - gh * (x[t] + xl[t])));
+        *(u2_t *)&Rt[(16 * t + d) * LC + w] = s.hi;
+        *(u2_t *)&Rl[(16 * t + d) * LC + w] = s.lo;
       }
-    if (CKPT)
-#pragma unroll
-      for (int i = 0; i < KTW; ++i) hs[i] = frag_of<VB, false>(Ht, LK, 16 * S::kt(wv, i));
-#pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) kT[i][kb] = ld8_steps(ks, LK, 32 * kb, 16 * S::kt(wv, i));
-#pragma unroll
-    for (int t = 0; t < VT; ++t) y[t] = u[t] = ul[t] = zero;
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      u[t] = mfma_k32(Tf[0], rh[t][0], u[t]);
-      ul[t] = mfma_k32(Tf[1], rh[t][0], ul[t]);
-      ul[t] = mfma_k32(Tf[0], rl[t][0], ul[t]);
-      u[t] = mfma_k32(Tf[2], rh[t][1], u[t]);
-      ul[t] = mfma_k32(Tf[3], rh[t][1], ul[t]);
-      ul[t] = mfma_k32(Tf[2], rl[t][1], ul[t]);
-    }
-    hold();
-    fetch2(next);
-    hold();
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      settle(u[t]);
-      settle(ul[t]);
-      const f4_t uu = u[t] + ul[t];
-      const Pair4 s = split4(gl * uu);
-      *(u2_t *)&Wt[(16 * t + d) * LC + w] = s.hi;
-      *(u2_t *)&Wl[(16 * t + d) * LC + w] = s.lo;
-      *(u2_t *)&Ut[(16 * t + d) * LC + w] = pack4_h(uu);
-    }
-    lds_barrier();
-    // H = e^{G_C} H + K^T W: D[row][column];  y = e^G (Q H)^T + (P U)^T
-    h8_t wh[VTW][2], wl[VTW][2], uf[VT][2], us;
-    const float gy = two_to(eh + qx) * g1, rp = two_to(er + ep), rus = two_to(er + kx - eh);
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) {
-        const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
-        wh[j][kb] = ld8(Wt + o);
-        wl[j][kb] = ld8(Wl + o);
-      }
-    if (Y) {
-      h8_t qf[KB];
-      rows_to_h8<FAR>(nq, eq, qf);
-#pragma unroll
-      for (int i = 0; i < KB; ++i)
-#pragma unroll
-        for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf[i], y[t]);
-    }
-    f4_t kw[KTW][VTW], hg[KTW][VTW];
-#pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) hg[i][j] = gc * H[i][j];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < KTW; ++i)
-#pragma unroll
-        for (int j = 0; j < VTW; ++j) {
-          kw[i][j] = mfma_k32(kT[i][kb], wl[j][kb], kb ? kw[i][j] : zero);
-          kw[i][j] = mfma_k32(kT[i][kb], wh[j][kb], kw[i][j]);
-        }
-#pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) {
-        settle(kw[i][j]);
-        H[i][j] = fma4(rus, kw[i][j], hg[i][j]);
-      }
-    if (Y) {
+      lds_barrier();
+      // U = T R: D[step][column];  off the chain (Q H)^T: D[column][step]
+      h8_t rh[VT][2], rl[VT][2], hs[KTW], kT[KTW][2];
+      f4_t y[VT], u[VT], ul[VT];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int t = 0; t < VT; ++t) uf[t][kb] = ld8(Ut + (16 * t + d) * LC + 32 * kb + 8 * g4);
+        for (int t = 0; t < VT; ++t) {
+          const int o = (16 * t + d) * LC + 32 * kb + 8 * g4;
+          rh[t][kb] = ld8(Rt + o);
+          rl[t][kb] = ld8(Rl + o);
+        }
+      if (CKPT)
+#pragma unroll
+        for (int i = 0; i < KTW; ++i) hs[i] = frag_of<VB, false>(Ht, LK, 16 * S::kt(wv, i));
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) kT[i][kb] = ld8_steps(ks, LK, 32 * kb, 16 * S::kt(wv, i));
+#pragma unroll
+      for (int t = 0; t < VT; ++t) y[t] = u[t] = ul[t] = zero;
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
-        u[t] = mfma_k32(uf[t][0], Pf[0], zero);
-        u[t] = mfma_k32(uf[t][1], Pf[1], u[t]);
+        u[t] = mfma_k32(Tf[0], rh[t][0], u[t]);
+        ul[t] = mfma_k32(Tf[1], rh[t][0], ul[t]);
+        ul[t] = mfma_k32(Tf[0], rl[t][0], ul[t]);
+        u[t] = mfma_k32(Tf[2], rh[t][1], u[t]);
+        ul[t] = mfma_k32(Tf[3], rh[t][1], ul[t]);
+        ul[t] = mfma_k32(Tf[2], rl[t][1], ul[t]);
       }
       hold();
-      fetch3(next);
+      fetch2(next);
       hold();
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
         settle(u[t]);
-        y[t] = gy * y[t] + rp * u[t];
+        settle(ul[t]);
+        const f4_t uu = u[t] + ul[t];
+        const Pair4 s = split4(gl * uu);
+        *(u2_t *)&Wt[(16 * t + d) * LC + w] = s.hi;
+        *(u2_t *)&Wl[(16 * t + d) * LC + w] = s.lo;
+        *(u2_t *)&Ut[(16 * t + d) * LC + w] = pack4_h(uu);
       }
-    }
-    if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
-    take1(far);
-    if (Y) {
-      const auto o = in.o.at(ch);
+      lds_barrier();
+      // H = e^{G_C} H + K^T W: D[row][column];  y = e^G (Q H)^T + (P U)^T
+      h8_t wh[VTW][2], wl[VTW][2], uf[VT][2], us;
+      const float gy = two_to(eh + qx) * g1, rp = two_to(er + ep), rus = two_to(er + kx - eh);
 #pragma unroll
-      for (int t = 0; t < VT; ++t)
-        buf_st(o, oy + 32 * t, u2_t{pack2_bf16(y[t][0], y[t][1]), pack2_bf16(y[t][2], y[t][3])});
-    }
-    if (CKPT) {
-      const size_t at = (size_t)unit * chunks + ch;
-      if (KT >= 4 || wv < KT)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < KTW; ++i) *(h8_t *)(states + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
-      *(h8_t *)(rows_u + at * C * a.V + frag_at<VB>(part, 4, wv)) = us;
-      // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
-      __builtin_amdgcn_raw_buffer_store_b32(lane ? er : eh, __builtin_amdgcn_make_buffer_rsrc(exps + (at * (a.V / VB) + part) * 2,
-                                            0, 8, 0x00027000), 4 * (int)threadIdx.x, 0, 0);
+        for (int j = 0; j < VTW; ++j) {
+          const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
+          wh[j][kb] = ld8(Wt + o);
+          wl[j][kb] = ld8(Wl + o);
+        }
+      if (Y) {
+        h8_t qf[KB];
+        rows_to_h8<FAR>(nq, eq, qf);
+#pragma unroll
+        for (int i = 0; i < KB; ++i)
+#pragma unroll
+          for (int t = 0; t < VT; ++t) y[t] = mfma_k32(hh[t][i], qf[i], y[t]);
+      }
+      f4_t kw[KTW][VTW], hg[KTW][VTW];
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) hg[i][j] = gc * H[i][j];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < KTW; ++i)
+#pragma unroll
+          for (int j = 0; j < VTW; ++j) {
+            kw[i][j] = mfma_k32(kT[i][kb], wl[j][kb], kb ? kw[i][j] : zero);
+            kw[i][j] = mfma_k32(kT[i][kb], wh[j][kb], kw[i][j]);
+          }
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          settle(kw[i][j]);
+          H[i][j] = fma4(rus, kw[i][j], hg[i][j]);
+        }
+      if (Y) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int t = 0; t < VT; ++t) uf[t][kb] = ld8(Ut + (16 * t + d) * LC + 32 * kb + 8 * g4);
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          u[t] = mfma_k32(uf[t][0], Pf[0], zero);
+          u[t] = mfma_k32(uf[t][1], Pf[1], u[t]);
+        }
+        hold();
+        fetch3(next);
+        hold();
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          settle(u[t]);
+          y[t] = gy * y[t] + rp * u[t];
+        }
+      }
+      if (CKPT) us = frag_of<VB, true>(Ut, LC, wv);
+      take1(far);
+      if (Y) {
+        const auto o = in.o.at(ch);
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+          buf_st(o, oy + 32 * t, u2_t{pack2_bf16(y[t][0], y[t][1]), pack2_bf16(y[t][2], y[t][3])});
+      }
+      if (CKPT) {
+        const size_t at = (size_t)unit * chunks + ch;
+        if (KT >= 4 || wv < KT)
+#pragma unroll
+          for (int i = 0; i < KTW; ++i) *(h8_t *)(states + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
+        *(h8_t *)(rows_u + at * C * a.V + frag_at<VB>(part, 4, wv)) = us;
+        // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
+        __builtin_amdgcn_raw_buffer_store_b32(lane ? er : eh, __builtin_amdgcn_make_buffer_rsrc(exps + (at * (a.V / VB) + part) * 2,
+                                              0, 8, 0x00027000), 4 * (int)threadIdx.x, 0, 0);
+      }
+      ++ch;
+      if (!FAR && is_far()) break;
     }
-    ++ch;
-    if (!FAR && is_far()) break;
-   }
-   return ch;
+    return ch;
   };
   int ch = p.c0;
   if (ch < p.c1 && !is_far()) ch = run_chunks(std::false_type(), ch);
@@ -1079,215 +1079,215 @@ __global__ void __launch_bounds__(256, 2)
   auto is_far = [&]() { return far_key(ek) || far_query(eq); };
   // the chunks from ch down, as in the forward
   auto run_chunks = [&](auto far, int ch) __attribute__((always_inline)) {
-   constexpr bool FAR = decltype(far)::value;
-   while (ch >= 0) {
-    const int next = max(ch - 1, 0), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
-    put_in();
-#pragma unroll
-    for (int i = 0; i < KB; ++i) {
-      *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
-      *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = qf[i];
-    }
-    top_of_wave(red, D, yf, wv);
-    lds_barrier();  // (of the chunk before only Z may still be read)
-    // dU = P^T dY + e^{G_C - G} K dH: D[step][column]
-    const uint32_t tops = top_of_all(red);
-    h8_t hh[VT][KB], hl[VT][KB], yy[VT][2];
-    auto get_in = [&]() {
-#pragma unroll
-      for (int i = 0; i < KB; ++i)
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
-          hh[t][i] = ld8(Ht + o);
-          hl[t][i] = ld8(Hl + o);
-        }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int t = 0; t < VT; ++t) yy[t][kb] = ld8(Yt + (16 * t + d) * LC + 32 * kb + 8 * g4);
-    };
-    f4_t u[VT], ul[VT], py[VT];
-    auto products = [&]() {
-#pragma unroll
-      for (int t = 0; t < VT; ++t) u[t] = ul[t] = py[t] = zero;
-#pragma unroll
-      for (int i = 0; i < KB; ++i)
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          u[t] = mfma_k32(kf[i], hh[t][i], u[t]);
-          ul[t] = mfma_k32(kf[i], hl[t][i], ul[t]);
-        }
-#pragma unroll
-      for (int t = 0; t < VT; ++t) {
-        py[t] = mfma_k32(Pf[0], yy[t][1], py[t]);
-        py[t] = mfma_k32(Pf[1], yy[t][1], py[t]);
-        py[t] = mfma_k32(Pf[2], yy[t][0], py[t]);
-        py[t] = mfma_k32(Pf[3], yy[t][0], py[t]);
-      }
-    };
-    get_in();
-    fetch1(next);
-    products();
-    f4_t glz = two_to(ed + kx - ez) * gl;
-    float pz = two_to(ey + ep - ez);
-    int td = ed + top_exponent(tops >> 16), ty_ = top_exponent(tops), tz = scale_of_z(td, ty_);
-    int want = scale_of_dh(td, ty_, tz);
-    if (not_finite(tops) | (want < ed - 2) | (want > ed + 13) | (ty_ < ey - 2) | (ty_ > ey + 13) | (tz < ez - 3) |
-        (tz > ez + 4)) {  // (the same in all waves)
-      measure(td, ey);
-      ez = scale_of_z(td, ey);
-      rescale(scale_of_dh(td, ey, ez));
+    constexpr bool FAR = decltype(far)::value;
+    while (ch >= 0) {
+      const int next = max(ch - 1, 0), kx = FAR ? ek : 0, qx = FAR ? eq : 0;
       put_in();
-      lds_barrier();
-      get_in();
-      products();
-      glz = two_to(ed + kx - ez) * gl;
-      pz = two_to(ey + ep - ez);
-    }
-    hold();
-    fetch2(next);
-    hold();
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      settle(u[t]);
-      settle(ul[t]);
-      settle(py[t]);
-      const Pair4 x = split4(glz * (u[t] + ul[t]) + pz * py[t]);
-      *(u2_t *)&Ut[(16 * t + d) * LC + w] = x.hi;
-      *(u2_t *)&Ul[(16 * t + d) * LC + w] = x.lo;
-    }
-    // (what Q^T e^G dY needs)
-    h8_t hs[KTW], xT[KTW][2], wh[VTW][2], wl[VTW][2];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) {
-        const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
-        wh[j][kb] = ld8(Wt + o);
-        wl[j][kb] = ld8(Wl + o);
+      for (int i = 0; i < KB; ++i) {
+        *(h8_t *)&ks[(16 * wv + d) * LK + 32 * i + 8 * g4] = kf[i];
+        *(h8_t *)&qs[(16 * wv + d) * LK + 32 * i + 8 * g4] = qf[i];
       }
+      top_of_wave(red, D, yf, wv);
+      lds_barrier();  // (of the chunk before only Z may still be read)
+      // dU = P^T dY + e^{G_C - G} K dH: D[step][column]
+      const uint32_t tops = top_of_all(red);
+      h8_t hh[VT][KB], hl[VT][KB], yy[VT][2];
+      auto get_in = [&]() {
 #pragma unroll
-      for (int i = 0; i < KTW; ++i) xT[i][kb] = ld8_steps(qs, LK, 32 * kb, 16 * S::kt(wv, i));
-    }
+        for (int i = 0; i < KB; ++i)
 #pragma unroll
-    for (int i = 0; i < KTW; ++i) hs[i] = frag_of<VB, false>(Ht, LK, 16 * S::kt(wv, i));
-    lds_barrier();
-    // Z = T^T dU as D[step][column] for the state, and as D[column][step] for what is written
-    h8_t uh[VT][2], uo[VT][2];
+          for (int t = 0; t < VT; ++t) {
+            const int o = (16 * t + d) * LK + 32 * i + 8 * g4;
+            hh[t][i] = ld8(Ht + o);
+            hl[t][i] = ld8(Hl + o);
+          }
 #pragma unroll
-    for (int kb = 1; kb >= 0; --kb)
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int t = 0; t < VT; ++t) yy[t][kb] = ld8(Yt + (16 * t + d) * LC + 32 * kb + 8 * g4);
+      };
+      f4_t u[VT], ul[VT], py[VT];
+      auto products = [&]() {
+#pragma unroll
+        for (int t = 0; t < VT; ++t) u[t] = ul[t] = py[t] = zero;
+#pragma unroll
+        for (int i = 0; i < KB; ++i)
+#pragma unroll
+          for (int t = 0; t < VT; ++t) {
+            u[t] = mfma_k32(kf[i], hh[t][i], u[t]);
+            ul[t] = mfma_k32(kf[i], hl[t][i], ul[t]);
+          }
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          py[t] = mfma_k32(Pf[0], yy[t][1], py[t]);
+          py[t] = mfma_k32(Pf[1], yy[t][1], py[t]);
+          py[t] = mfma_k32(Pf[2], yy[t][0], py[t]);
+          py[t] = mfma_k32(Pf[3], yy[t][0], py[t]);
+        }
+      };
+      get_in();
+      fetch1(next);
+      products();
+      f4_t glz = two_to(ed + kx - ez) * gl;
+      float pz = two_to(ey + ep - ez);
+      int td = ed + top_exponent(tops >> 16), ty_ = top_exponent(tops), tz = scale_of_z(td, ty_);
+      int want = scale_of_dh(td, ty_, tz);
+      if (not_finite(tops) | (want < ed - 2) | (want > ed + 13) | (ty_ < ey - 2) | (ty_ > ey + 13) | (tz < ez - 3) |
+          (tz > ez + 4)) {  // (the same in all waves)
+        measure(td, ey);
+        ez = scale_of_z(td, ey);
+        rescale(scale_of_dh(td, ey, ez));
+        put_in();
+        lds_barrier();
+        get_in();
+        products();
+        glz = two_to(ed + kx - ez) * gl;
+        pz = two_to(ey + ep - ez);
+      }
+      hold();
+      fetch2(next);
+      hold();
 #pragma unroll
       for (int t = 0; t < VT; ++t) {
-        const int o = (16 * t + d) * LC + 32 * kb + 8 * g4;
-        uh[t][kb] = ld8(Ut + o);
-        uo[t][kb] = ld8(Ul + o);
+        settle(u[t]);
+        settle(ul[t]);
+        settle(py[t]);
+        const Pair4 x = split4(glz * (u[t] + ul[t]) + pz * py[t]);
+        *(u2_t *)&Ut[(16 * t + d) * LC + w] = x.hi;
+        *(u2_t *)&Ul[(16 * t + d) * LC + w] = x.lo;
       }
-    f4_t acc[KTW][VTW];
+      // (what Q^T e^G dY needs)
+      h8_t hs[KTW], xT[KTW][2], wh[VTW][2], wl[VTW][2];
 #pragma unroll
-    for (int i = 0; i < KTW; ++i)
+      for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-      for (int j = 0; j < VTW; ++j) {
-        acc[i][j] = zero;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], acc[i][j]);
-          acc[i][j] = mfma_k32(xT[i][kb], wh[j][kb], acc[i][j]);
+        for (int j = 0; j < VTW; ++j) {
+          const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
+          wh[j][kb] = ld8(Wt + o);
+          wl[j][kb] = ld8(Wl + o);
         }
-      }
-    f4_t x[VT], xl[VT], z[VT];
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      x[t] = mfma_k32(Tf[0], uh[t][1], zero);
-      xl[t] = mfma_k32(Tf[1], uh[t][1], zero);
-      xl[t] = mfma_k32(Tf[0], uo[t][1], xl[t]);
-      x[t] = mfma_k32(Tf[2], uh[t][0], x[t]);
-      xl[t] = mfma_k32(Tf[3], uh[t][0], xl[t]);
-      xl[t] = mfma_k32(Tf[2], uo[t][0], xl[t]);
-    }
-    const f4_t bg = -two_to(-eb) * (be * ge);
-#pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      settle(x[t]);
-      settle(xl[t]);
-      const Pair4 y = split4(bg * (x[t] + xl[t]));
-      *(u2_t *)&Zt[(16 * t + d) * LC + w] = y.hi;
-      *(u2_t *)&Zl[(16 * t + d) * LC + w] = y.lo;
-    }
-#pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) xT[i][kb] = ld8_steps(ks, LK, 32 * kb, 16 * S::kt(wv, i));
-    lds_barrier();
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) {
-        const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
-        wh[j][kb] = ld8(Zt + o);
-        wl[j][kb] = ld8(Zl + o);
+        for (int i = 0; i < KTW; ++i) xT[i][kb] = ld8_steps(qs, LK, 32 * kb, 16 * S::kt(wv, i));
       }
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      z[t] = mfma_k32(uo[t][1], Tf[0], zero);
-      z[t] = mfma_k32(uh[t][1], Tf[1], z[t]);
-      z[t] = mfma_k32(uh[t][1], Tf[0], z[t]);
-      z[t] = mfma_k32(uo[t][0], Tf[2], z[t]);
-      z[t] = mfma_k32(uh[t][0], Tf[3], z[t]);
-      z[t] = mfma_k32(uh[t][0], Tf[2], z[t]);
-    }
-    hold();
-    fetch3(next);
-    hold();
+      for (int i = 0; i < KTW; ++i) hs[i] = frag_of<VB, false>(Ht, LK, 16 * S::kt(wv, i));
+      lds_barrier();
+      // Z = T^T dU as D[step][column] for the state, and as D[column][step] for what is written
+      h8_t uh[VT][2], uo[VT][2];
 #pragma unroll
-    for (int t = 0; t < VT; ++t) settle(z[t]);
-    const float backq = om * two_to(ey + qx - ed), backk = om * two_to(ez + eb + kx - ed);
+      for (int kb = 1; kb >= 0; --kb)
 #pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) {
-        settle(acc[i][j]);
-        D[i][j] = gc * D[i][j] + backq * acc[i][j];
-      }
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+        for (int t = 0; t < VT; ++t) {
+          const int o = (16 * t + d) * LC + 32 * kb + 8 * g4;
+          uh[t][kb] = ld8(Ut + o);
+          uo[t][kb] = ld8(Ul + o);
+        }
+      f4_t acc[KTW][VTW];
 #pragma unroll
       for (int i = 0; i < KTW; ++i)
 #pragma unroll
         for (int j = 0; j < VTW; ++j) {
-          acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], kb ? acc[i][j] : zero);
-          acc[i][j] = mfma_k32(xT[i][kb], wh[j][kb], acc[i][j]);
+          acc[i][j] = zero;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+            acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], acc[i][j]);
+            acc[i][j] = mfma_k32(xT[i][kb], wh[j][kb], acc[i][j]);
+          }
+        }
+      f4_t x[VT], xl[VT], z[VT];
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        x[t] = mfma_k32(Tf[0], uh[t][1], zero);
+        xl[t] = mfma_k32(Tf[1], uh[t][1], zero);
+        xl[t] = mfma_k32(Tf[0], uo[t][1], xl[t]);
+        x[t] = mfma_k32(Tf[2], uh[t][0], x[t]);
+        xl[t] = mfma_k32(Tf[3], uh[t][0], xl[t]);
+        xl[t] = mfma_k32(Tf[2], uo[t][0], xl[t]);
+      }
+      const f4_t bg = -two_to(-eb) * (be * ge);
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        settle(x[t]);
+        settle(xl[t]);
+        const Pair4 y = split4(bg * (x[t] + xl[t]));
+        *(u2_t *)&Zt[(16 * t + d) * LC + w] = y.hi;
+        *(u2_t *)&Zl[(16 * t + d) * LC + w] = y.lo;
+      }
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) xT[i][kb] = ld8_steps(ks, LK, 32 * kb, 16 * S::kt(wv, i));
+      lds_barrier();
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          const int o = (16 * S::vt(wv, j) + d) * LC + 32 * kb + 8 * g4;
+          wh[j][kb] = ld8(Zt + o);
+          wl[j][kb] = ld8(Zl + o);
         }
 #pragma unroll
-    for (int i = 0; i < KTW; ++i)
-#pragma unroll
-      for (int j = 0; j < VTW; ++j) {
-        settle(acc[i][j]);
-        D[i][j] = fma4(backk, acc[i][j], D[i][j]);
+      for (int t = 0; t < VT; ++t) {
+        z[t] = mfma_k32(uo[t][1], Tf[0], zero);
+        z[t] = mfma_k32(uh[t][1], Tf[1], z[t]);
+        z[t] = mfma_k32(uh[t][1], Tf[0], z[t]);
+        z[t] = mfma_k32(uo[t][0], Tf[2], z[t]);
+        z[t] = mfma_k32(uh[t][0], Tf[3], z[t]);
+        z[t] = mfma_k32(uh[t][0], Tf[2], z[t]);
       }
-    const float bz = b1 * two_to(ez);
-    take1(far);
-    const size_t at = (size_t)unit * chunks + ch;
-    const auto o = in.o.at(ch);
+      hold();
+      fetch3(next);
+      hold();
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
-      // (a lane's four columns are half of the eight that the operand's lane d + 16 (column / 8) holds)
-      const int c = (VB == 32 ? 0 : 16 * (part & 1)) + 16 * t + 4 * g4, v32 = VB == 32 ? part : part >> 1;
-      *(u2_t *)(rows_z + at * C * a.V + ((size_t)(v32 * 4 + wv) * 64 + d + 16 * (c >> 3)) * 8 + (c & 7)) = pack4_h(z[t]);
-      const f4_t dv = bz * z[t];
-      buf_st(o, oo + 32 * t, u2_t{pack2_bf16(dv[0], dv[1]), pack2_bf16(dv[2], dv[3])});
+      for (int t = 0; t < VT; ++t) settle(z[t]);
+      const float backq = om * two_to(ey + qx - ed), backk = om * two_to(ez + eb + kx - ed);
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          settle(acc[i][j]);
+          D[i][j] = gc * D[i][j] + backq * acc[i][j];
+        }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < KTW; ++i)
+#pragma unroll
+          for (int j = 0; j < VTW; ++j) {
+            acc[i][j] = mfma_k32(xT[i][kb], wl[j][kb], kb ? acc[i][j] : zero);
+            acc[i][j] = mfma_k32(xT[i][kb], wh[j][kb], acc[i][j]);
+          }
+#pragma unroll
+      for (int i = 0; i < KTW; ++i)
+#pragma unroll
+        for (int j = 0; j < VTW; ++j) {
+          settle(acc[i][j]);
+          D[i][j] = fma4(backk, acc[i][j], D[i][j]);
+        }
+      const float bz = b1 * two_to(ez);
+      take1(far);
+      const size_t at = (size_t)unit * chunks + ch;
+      const auto o = in.o.at(ch);
+#pragma unroll
+      for (int t = 0; t < VT; ++t) {
+        // (a lane's four columns are half of the eight that the operand's lane d + 16 (column / 8) holds)
+        const int c = (VB == 32 ? 0 : 16 * (part & 1)) + 16 * t + 4 * g4, v32 = VB == 32 ? part : part >> 1;
+        *(u2_t *)(rows_z + at * C * a.V + ((size_t)(v32 * 4 + wv) * 64 + d + 16 * (c >> 3)) * 8 + (c & 7)) = pack4_h(z[t]);
+        const f4_t dv = bz * z[t];
+        buf_st(o, oo + 32 * t, u2_t{pack2_bf16(dv[0], dv[1]), pack2_bf16(dv[2], dv[3])});
+      }
+      if (KT >= 4 || wv < KT)
+#pragma unroll
+        for (int i = 0; i < KTW; ++i) *(h8_t *)(dstates + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
+      // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
+      __builtin_amdgcn_raw_buffer_store_b128(u4_t{(uint32_t)ed, (uint32_t)ez, (uint32_t)ey, 0u}, __builtin_amdgcn_make_buffer_rsrc(
+                                             exps + at * (a.V / VB) + part, 0, 16, 0x00027000), 16 * (int)threadIdx.x, 0, 0);
+      if (!own_z<K, VB>()) lds_barrier();
+      --ch;
+      if (!FAR && is_far()) break;
     }
-    if (KT >= 4 || wv < KT)
-#pragma unroll
-      for (int i = 0; i < KTW; ++i) *(h8_t *)(dstates + at * K * a.V + frag_at<VB>(part, KT, S::kt(wv, i))) = hs[i];
-    // (lanes behind the buffer's end write nothing; a branch would make the next loads wait for all stores)
-    __builtin_amdgcn_raw_buffer_store_b128(u4_t{(uint32_t)ed, (uint32_t)ez, (uint32_t)ey, 0u}, __builtin_amdgcn_make_buffer_rsrc(
-                                           exps + at * (a.V / VB) + part, 0, 16, 0x00027000), 16 * (int)threadIdx.x, 0, 0);
-    if (!own_z<K, VB>()) lds_barrier();
-    --ch;
-    if (!FAR && is_far()) break;
-   }
-   return ch;
+    return ch;
   };
   int ch = chunks - 1;
   if (ch >= 0 && !is_far()) ch = run_chunks(std::false_type(), ch);
